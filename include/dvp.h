@@ -54,7 +54,8 @@ typedef enum {
   DVP_ERR_CUDA = 4         /* a CUDA runtime call failed                     */
 } dvp_status;
 
-typedef enum { DVP_F32 = 0, DVP_BF16 = 1, DVP_F16 = 2 } dvp_dtype;
+/* DVP_E4M3: 8-bit floating point (4 exponent bits, 3 of the significand, largest value 448), where an entry point says so */
+typedef enum { DVP_F32 = 0, DVP_BF16 = 1, DVP_F16 = 2, DVP_E4M3 = 3 } dvp_dtype;
 typedef enum { DVP_ID_I64 = 0, DVP_ID_I32 = 1 } dvp_id_dtype;
 
 /* bits of the per-token flags byte */
@@ -80,7 +81,7 @@ enum {
  */
 enum { DVP_MODE_FINITE_MASK = 1, DVP_MODE_THRESHOLD_IN_LOGITS_DTYPE = 2 };
 
-enum { DVP_ENTRY_FORWARD = 0, DVP_ENTRY_BACKWARD = 1, DVP_ENTRY_FUSED_LMHEAD = 2 };
+enum { DVP_ENTRY_FORWARD = 0, DVP_ENTRY_BACKWARD = 1, DVP_ENTRY_FUSED_LMHEAD = 2, DVP_ENTRY_RMS_NORM_BACKWARD = 3 };
 
 /*
  * `weight_kind` of dvp_forward_args: the per-token upstream gradient is
@@ -513,6 +514,82 @@ int dvp_row_wait_status(uint32_t *status_out);
  * in for a memory checker.  Errors: DVP_ERR_INVALID_ARG (NULL), DVP_ERR_CUDA.
  */
 int dvp_debug_bounds_status(uint32_t *status_out);
+
+/*
+ * ---- the stage before the logits ------------------------------------------------------
+ * What stands between a model's last layer and the logits this library works on: the final
+ * norm, and on the rollout's side an LM head in 8 bits.  The paper has no counterpart; it
+ * names low-precision rollouts as a source of the mismatch it treats (Sec. 4).  An 8-bit
+ * matrix holds e4m3 values q and float32 scales c, one for each block of 128 columns (of
+ * activations, per row; of weights, for blocks of 128 rows), and stands for c q.
+ *
+ * dvp_rms_norm -- root-mean-square norm, with the residual's addition:
+ *   h = x + residual,  s = (mean_j h_j^2 + eps)^(-1/2),  y_j = h_j s weight_j
+ * in float32 from the stored values; every output is rounded once.
+ *
+ *   x, residual   device [T, ld] of x_dtype; residual may be NULL
+ *   weight        device [H] of x_dtype or DVP_F32 (weight_dtype)
+ *   residual_out  device [T, ld_residual_out] of x_dtype or NULL: h; may take the place of x or residual (the same
+ *                 base and stride)
+ *   out           device [T, ld_out] of out_dtype: y; DVP_F32, DVP_BF16, DVP_F16, or DVP_E4M3 with `scale`.  In x_dtype
+ *                 it may take the place of x, or of a residual that residual_out does not take the place of
+ *   scale         device [T, ld_scale] float32, ld_scale >= ceil(H / 128), with DVP_E4M3 only: for each row and block
+ *                 of 128 columns c = max(max |y|, 2^-96) / 448; out holds y / c, to nearest.  A block with NaN keeps its
+ *                 NaN entries, one with an infinity has c infinite and entries of zero and NaN
+ *   rstd          device [T] float32 or NULL: s, for dvp_rms_norm_backward
+ * Rows of any width, stride and alignment to their element; bases and strides of 32 bytes and a width that is a multiple of
+ * 8 are the fast way.  Needs no workspace.  T = 0 is a valid no-op.  Errors: DVP_ERR_INVALID_ARG (null pointers, negative
+ * sizes, H < 1, strides below the width, eps negative or not finite, scale without DVP_E4M3 or the reverse),
+ * DVP_ERR_UNSUPPORTED (dtypes, T or H >= 2^31 - 256).
+ */
+typedef struct {
+  uint32_t struct_size;
+  int32_t x_dtype, weight_dtype, out_dtype;
+  int64_t T, H;
+  int64_t ld_x, ld_residual, ld_residual_out, ld_out, ld_scale;
+  double eps;
+  const void *x, *residual, *weight;
+  void *residual_out, *out;
+  float *scale, *rstd;
+  void *stream;
+} dvp_rms_norm_args;
+
+int dvp_rms_norm(const dvp_rms_norm_args *args);
+
+/*
+ * dvp_rms_norm_backward -- from dy = dLoss/dy (the fused LM head's d_hidden, for one), with g = dy weight:
+ *   d_x = s (g - h s^2 mean_j(g_j h_j)) (+ d_residual),   d_weight (+)= sum_t dy_t h_t s_t
+ * d_x is the gradient of x and of the residual; d_residual is what reaches h by its other way, past the norm.
+ *
+ *   dy            device [T, ld_dy] of dy_dtype (DVP_F32, DVP_BF16, DVP_F16)
+ *   h             device [T, ld_h] of h_dtype: what the norm was taken of (residual_out, or x without a residual)
+ *   weight        device [H] of h_dtype or DVP_F32
+ *   rstd          device [T] float32 as written by dvp_rms_norm
+ *   d_residual    device [T, ld_d_residual] of h_dtype or NULL
+ *   d_x           device [T, ld_d_x] of h_dtype or NULL; may take the place of dy or d_residual (the same type, base, stride)
+ *   d_weight      device [H] float32 or NULL; overwritten, or added to when accumulate_dw != 0
+ *   workspace     device, 256-byte aligned, dvp_workspace_bytes(DVP_ENTRY_RMS_NORM_BACKWARD, args) bytes; none without d_weight.
+ *                 The sum over the tokens has a fixed order: reruns are bit-identical
+ * Layouts and errors as in dvp_rms_norm; DVP_ERR_WORKSPACE.  T = 0 clears d_weight (accumulate_dw: leaves it).
+ */
+typedef struct {
+  uint32_t struct_size;
+  int32_t h_dtype, weight_dtype, dy_dtype;
+  int64_t T, H;
+  int64_t ld_dy, ld_h, ld_d_residual, ld_d_x;
+  const void *dy, *h, *weight;
+  const float *rstd;
+  const void *d_residual;
+  void *d_x;
+  float *d_weight;
+  void *workspace;
+  size_t workspace_bytes;
+  void *stream;
+  int32_t accumulate_dw;
+  uint32_t reserved_;
+} dvp_rms_norm_backward_args;
+
+int dvp_rms_norm_backward(const dvp_rms_norm_backward_args *args);
 
 /*
  * Bytes of device workspace the entry point needs for `args` (a pointer to

@@ -20,10 +20,10 @@ LIB_PATH = os.path.join(_HERE, "libdvp_b200.so")
 BOUNDS_LIB_PATH = os.path.join(_HERE, "libdvp_b200_bounds.so")   # the bounds-checking build
 
 DVP_OK, DVP_ERR_INVALID_ARG, DVP_ERR_UNSUPPORTED, DVP_ERR_WORKSPACE, DVP_ERR_CUDA = range(5)
-DVP_F32, DVP_BF16, DVP_F16 = 0, 1, 2
+DVP_F32, DVP_BF16, DVP_F16, DVP_E4M3 = 0, 1, 2, 3
 DVP_ID_I64, DVP_ID_I32 = 0, 1
 DVP_FLAG_IN_TRAIN, DVP_FLAG_IN_INFER, DVP_FLAG_NO_ID, DVP_FLAG_BAD_ID = 1, 2, 64, 128
-DVP_ENTRY_FORWARD, DVP_ENTRY_BACKWARD, DVP_ENTRY_FUSED_LMHEAD = 0, 1, 2
+DVP_ENTRY_FORWARD, DVP_ENTRY_BACKWARD, DVP_ENTRY_FUSED_LMHEAD, DVP_ENTRY_RMS_NORM_BACKWARD = 0, 1, 2, 3
 DVP_STATIC_WORKSPACE_BYTES = 32 * 1024 * 1024
 DVP_MODE_FINITE_MASK, DVP_MODE_THRESHOLD_IN_LOGITS_DTYPE = 1, 2
 DVP_WEIGHT_NONE, DVP_WEIGHT_RATIO, DVP_WEIGHT_TRUNCATE, DVP_WEIGHT_MASK = 0, 1, 2, 3
@@ -31,9 +31,11 @@ DVP_WEIGHT_NONE, DVP_WEIGHT_RATIO, DVP_WEIGHT_TRUNCATE, DVP_WEIGHT_MASK = 0, 1, 
 EXPORTS = ("dvp_forward", "dvp_backward", "dvp_fused_lmhead_forward_backward",
            "dvp_fused_lmhead_forward_backward_static", "dvp_sequence_aggregate", "dvp_monitor", "dvp_gemm_tn",
            "dvp_workspace_bytes", "dvp_status_string", "dvp_version", "dvp_row_wait_status",
-           "dvp_static_workspace_status", "dvp_debug_bounds_status")
+           "dvp_static_workspace_status", "dvp_debug_bounds_status", "dvp_rms_norm", "dvp_rms_norm_backward")
 
 _DTYPES = {torch.float32: DVP_F32, torch.bfloat16: DVP_BF16, torch.float16: DVP_F16}
+_OUT_DTYPES = {**_DTYPES, torch.float8_e4m3fn: DVP_E4M3}
+FP8_BLOCK = 128   # columns, and rows of a weight, that share a scale
 _SIDE_FIELDS = ("max", "lse", "lse_safe", "logp", "logp_mp", "comp_mp", "count", "mask", "log_cov")
 
 
@@ -181,6 +183,58 @@ class MonitorArgs(ctypes.Structure):
     ]
 
 
+class RmsNormArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("x_dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("T", ctypes.c_int64),
+        ("H", ctypes.c_int64),
+        ("ld_x", ctypes.c_int64),
+        ("ld_residual", ctypes.c_int64),
+        ("ld_residual_out", ctypes.c_int64),
+        ("ld_out", ctypes.c_int64),
+        ("ld_scale", ctypes.c_int64),
+        ("eps", ctypes.c_double),
+        ("x", ctypes.c_void_p),
+        ("residual", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p),
+        ("residual_out", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("rstd", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class RmsNormBackwardArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("h_dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("dy_dtype", ctypes.c_int32),
+        ("T", ctypes.c_int64),
+        ("H", ctypes.c_int64),
+        ("ld_dy", ctypes.c_int64),
+        ("ld_h", ctypes.c_int64),
+        ("ld_d_residual", ctypes.c_int64),
+        ("ld_d_x", ctypes.c_int64),
+        ("dy", ctypes.c_void_p),
+        ("h", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p),
+        ("rstd", ctypes.c_void_p),
+        ("d_residual", ctypes.c_void_p),
+        ("d_x", ctypes.c_void_p),
+        ("d_weight", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p),
+        ("accumulate_dw", ctypes.c_int32),
+        ("reserved_", ctypes.c_uint32),
+    ]
+
+
 # The hot entry points are called with their argument structs packed in one go: setting the fields of a ctypes
 # structure one by one costs several microseconds a call.
 _FORWARD_PACK = struct.Struct("=I3i5qd5Q18Q3QIIfIffQ")
@@ -188,6 +242,10 @@ _BACKWARD_PACK = struct.Struct("=I3i4qd9QIIfI")
 _MONITOR_PACK = struct.Struct("=Ii4q7Q")
 _SEQUENCE_PACK = struct.Struct("=II2q2Qd9Q")
 _FUSED_PACK = struct.Struct("=Ii8qd7Qii18Q5QIff4xQ")
+_RMS_NORM_PACK = struct.Struct("=I3i7qd8Q")
+_RMS_NORM_BACKWARD_PACK = struct.Struct("=I3i6q10QiI")
+assert _RMS_NORM_PACK.size == ctypes.sizeof(RmsNormArgs)
+assert _RMS_NORM_BACKWARD_PACK.size == ctypes.sizeof(RmsNormBackwardArgs)
 assert _FUSED_PACK.size == ctypes.sizeof(FusedArgs)
 assert _FORWARD_PACK.size == ctypes.sizeof(ForwardArgs) and _BACKWARD_PACK.size == ctypes.sizeof(BackwardArgs)
 assert _MONITOR_PACK.size == ctypes.sizeof(MonitorArgs) and _SEQUENCE_PACK.size == ctypes.sizeof(SequenceArgs)
@@ -243,8 +301,11 @@ def load_library() -> ctypes.CDLL:
         lib.dvp_static_workspace_status.restype = ctypes.c_int
         lib.dvp_debug_bounds_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
         lib.dvp_debug_bounds_status.restype = ctypes.c_int
+        for name in ("dvp_rms_norm", "dvp_rms_norm_backward"):
+            lib[name].restype = ctypes.c_int
         lib.packed = {}   # the entry points that take a packed struct
-        for name in ("dvp_forward", "dvp_backward", "dvp_monitor", "dvp_sequence_aggregate"):
+        for name in ("dvp_forward", "dvp_backward", "dvp_monitor", "dvp_sequence_aggregate", "dvp_rms_norm",
+                     "dvp_rms_norm_backward"):
             fn = lib[name]   # a function object of its own, with its own argtypes
             fn.argtypes, fn.restype = [ctypes.c_char_p], ctypes.c_int
             lib.packed[name] = fn
@@ -348,6 +409,32 @@ _UINT32 = 0xffffffff
 def _int32(x) -> int:
     """The same for an int32_t."""
     return (int(x) + 0x80000000 & 0xffffffff) - 0x80000000
+
+
+def _check_same_device(like: torch.Tensor, **others):
+    for name, t in others.items():
+        if t is not None and t.device != like.device:
+            raise ValueError(f"{name} must live on {like.device}")
+
+
+def _on_device_of(t: torch.Tensor):
+    """The library launches on the current device: for the length of the block that is the tensor's."""
+    if t.get_device() == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(t.get_device())
+
+
+def _check_vector(name: str, x: torch.Tensor, n: int, dtypes):
+    if x.dim() != 1 or x.shape[0] != n or x.stride(0) != 1 and n > 1:
+        raise ValueError(f"{name} must be a contiguous vector of {n} elements")
+    if x.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}")
+
+
+def _check_like(name: str, x: torch.Tensor, shape, dtype):
+    _check_matrix(name, x)
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}")
 
 
 def _id_dtype(ids: torch.Tensor) -> int:
@@ -657,3 +744,83 @@ def dvp_monitor(train_logits: torch.Tensor, infer_logits: torch.Tensor, stream=N
         raise DvpError(st, "dvp_monitor")
     return SimpleNamespace(kl_infer_train=rows[0], kl_train_infer=rows[1], entropy_train=rows[2],
                            entropy_infer=rows[3])
+
+
+def dvp_rms_norm(x: torch.Tensor, weight: torch.Tensor, *, residual: torch.Tensor | None = None, eps: float = 1e-6,
+                 out_dtype: torch.dtype | None = None, residual_out: torch.Tensor | None = None, stream=None):
+    """Root-mean-square norm of ``x`` [T, H], or of ``x + residual``, times ``weight`` [H]: the norm before the LM head.
+
+    ``out_dtype`` is that of ``x`` unless given; with ``torch.float8_e4m3fn`` the result comes in 8 bits with a float32
+    scale for each row and block of 128 columns, as ``dvp_gemm_fp8`` takes it.  Returns a namespace with ``y``, ``scale``
+    [T, ceil(H / 128)] or None, ``residual`` (``x + residual`` in the type of ``x``, or None; written to ``residual_out``
+    where that is given, which may be ``x`` or ``residual``) and ``rstd`` [T] float32 for ``dvp_rms_norm_backward``."""
+    packed = load_library().packed
+    _check_matrix("x", x)
+    T, H = x.shape
+    out_dtype = out_dtype or x.dtype
+    if x.dtype not in _DTYPES or out_dtype not in _OUT_DTYPES:
+        raise TypeError("x must be float32, bfloat16 or float16, out_dtype one of these or float8_e4m3fn")
+    _check_vector("weight", weight, H, (x.dtype, torch.float32))
+    _check_same_device(x, weight=weight, residual=residual, residual_out=residual_out)
+    if residual is not None:
+        _check_like("residual", residual, (T, H), x.dtype)
+        if residual_out is None:
+            residual_out = x.new_empty((T, H))
+    if residual_out is not None:
+        _check_like("residual_out", residual_out, (T, H), x.dtype)
+    fp8 = out_dtype == torch.float8_e4m3fn
+    # 8-bit rows start on 16-byte boundaries, where the tensor cores' loads want them
+    y = x.new_empty((T, -(-H // 16) * 16), dtype=out_dtype)[:, :H] if fp8 else x.new_empty((T, H), dtype=out_dtype)
+    scale = x.new_empty((T, -(-H // FP8_BLOCK)), dtype=torch.float32) if fp8 else None
+    rstd = x.new_empty(T, dtype=torch.float32)
+    with _on_device_of(x):
+        st = packed["dvp_rms_norm"](_RMS_NORM_PACK.pack(
+            _RMS_NORM_PACK.size, _DTYPES[x.dtype], _DTYPES[weight.dtype], _OUT_DTYPES[out_dtype], T, H, x.stride(0),
+            residual.stride(0) if residual is not None else 0, residual_out.stride(0) if residual_out is not None else 0,
+            y.stride(0), scale.stride(0) if fp8 else 0, float(eps), x.data_ptr(), _address(residual), weight.data_ptr(),
+            _address(residual_out), y.data_ptr(), _address(scale), rstd.data_ptr(), _stream(stream)))
+    if st != DVP_OK:
+        raise DvpError(st, "dvp_rms_norm")
+    return SimpleNamespace(y=y, scale=scale, residual=residual_out, rstd=rstd)
+
+
+def dvp_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, *,
+                          d_residual: torch.Tensor | None = None, d_weight: torch.Tensor | None = None,
+                          accumulate_dw: bool = False, workspace: torch.Tensor | None = None, stream=None):
+    """The way back through ``dvp_rms_norm`` from ``dy`` = dLoss/dy (the float32 ``d_hidden`` of the fused LM head, or any
+    of the three types).  ``h`` is what the norm was taken of (its ``residual`` result, or ``x`` without a residual),
+    ``rstd`` its result, ``d_residual`` the gradient that reaches ``h`` past the norm.  Returns a namespace with ``d_x``
+    (in the type of ``h``; the gradient of ``x`` and of the residual) and ``d_weight`` [H] float32, added to the given one
+    with ``accumulate_dw``."""
+    lib = load_library()
+    _check_matrix("dy", dy)
+    _check_matrix("h", h)
+    T, H = h.shape
+    if dy.shape != h.shape:
+        raise ValueError("dy must match h in shape")
+    if h.dtype not in _DTYPES or dy.dtype not in _DTYPES:
+        raise TypeError("h and dy must be float32, bfloat16 or float16")
+    _check_vector("weight", weight, H, (h.dtype, torch.float32))
+    _check_vector("rstd", rstd, T, (torch.float32,))
+    _check_same_device(h, dy=dy, weight=weight, rstd=rstd, d_residual=d_residual, d_weight=d_weight, workspace=workspace)
+    if d_residual is not None:
+        _check_like("d_residual", d_residual, (T, H), h.dtype)
+    if d_weight is None:
+        if accumulate_dw:
+            raise ValueError("accumulate_dw needs d_weight")
+        d_weight = h.new_empty(H, dtype=torch.float32)
+    _check_vector("d_weight", d_weight, H, (torch.float32,))
+    d_x = h.new_empty((T, H))
+    fields = [_RMS_NORM_BACKWARD_PACK.size, _DTYPES[h.dtype], _DTYPES[weight.dtype], _DTYPES[dy.dtype], T, H, dy.stride(0),
+              h.stride(0), d_residual.stride(0) if d_residual is not None else 0, d_x.stride(0), dy.data_ptr(), h.data_ptr(),
+              weight.data_ptr(), rstd.data_ptr(), _address(d_residual), d_x.data_ptr(), d_weight.data_ptr(), 0, 0, 0,
+              int(bool(accumulate_dw)), 0]
+    if workspace is None:
+        need = lib.dvp_workspace_bytes(DVP_ENTRY_RMS_NORM_BACKWARD, _RMS_NORM_BACKWARD_PACK.pack(*fields))
+        workspace = h.new_empty(max(need, 256), dtype=torch.uint8)
+    with _on_device_of(h):
+        fields[17:20] = workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)
+        st = lib.packed["dvp_rms_norm_backward"](_RMS_NORM_BACKWARD_PACK.pack(*fields))
+    if st != DVP_OK:
+        raise DvpError(st, "dvp_rms_norm_backward")
+    return SimpleNamespace(d_x=d_x, d_weight=d_weight)

@@ -586,6 +586,9 @@ cudaError_t launch_backward_kernel(const BackwardParams &p, int logits_dtype, in
 // The last of three launches for a call (kOrderApart): log-ratios and flags from what the other two have left.
 cudaError_t launch_ratio_kernel(const RowParams &p, long long t0, long long n, cudaStream_t s);
 
+// dvp_workspace_bytes of dvp_rms_norm_backward (dvp_norm.cu).
+size_t rms_norm_backward_workspace(const void *args);
+
 // Synchronises the current device, reads the resident-row kernel's status word and clears it.
 cudaError_t read_and_clear_row_status(uint32_t *host_out);
 

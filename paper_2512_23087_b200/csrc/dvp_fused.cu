@@ -258,6 +258,7 @@ dvp_side_out offset_side(const dvp_side_out &o, long long r0, long long words) {
 extern "C" {
 
 size_t dvp_workspace_bytes(int entry_point, const void *args) {
+  if (entry_point == DVP_ENTRY_RMS_NORM_BACKWARD) return dvp::rms_norm_backward_workspace(args);
   if (entry_point != DVP_ENTRY_FUSED_LMHEAD || !args) return 0;
   const dvp_fused_args *a = static_cast<const dvp_fused_args *>(args);
   if (a->struct_size != sizeof(dvp_fused_args)) return 0;

@@ -1,0 +1,508 @@
+// Root-mean-square norm with the residual's addition, its output in the model's type or in 8 bits with a scale for each
+// block of 128 columns, and its backward pass.
+//
+//   h = x + r,  s = (mean h^2 + eps)^(-1/2),  y = h s w;      8 bits: c = max(max |y|, 2^-96) / 448 a block, q = e4m3(y / c)
+//   g = dy w,   dx = s (g - h s^2 mean(g h)) (+ dr),          dw = sum_t dy h s
+//
+// Both are bound by HBM: a row's threads hold it in registers between the sum and the output, so every matrix passes
+// once.  Rows that vectors of eight elements do not fit (width, stride or base) have kernels of their own, which read a row
+// twice, element by element.
+#include <cmath>
+
+#include "dvp_common.cuh"
+
+#include <cuda_fp8.h>
+
+namespace dvp {
+namespace norm {
+
+constexpr int kBlockCols = 128;  // columns that share a scale
+constexpr int kVec = 8;          // elements of a vector: 16 bytes of a 16-bit type, 32 of float32, 8 of e4m3
+constexpr float kFp8Max = 448.f;
+constexpr float kLeastAmax = 1.262177448e-29f;  // 2^-96: a block of zeros has a scale that can be divided by
+constexpr int kMaxPartials = 592;               // rows of partial sums of dw: four blocks an SM
+
+struct Params {
+  const void *x, *r, *w;
+  void *r_out, *out;
+  float *scale, *rstd;
+  long long T, H, ld_x, ld_r, ld_r_out, ld_out, ld_scale;
+  float inv_h, eps;
+  int w_f32;
+};
+
+// Eight neighbouring elements.  Not through the read-only path: an output may take the place of an input, whose elements
+// the same thread has read.
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "l"(p)
+                 : "memory");
+  } else {
+    uint4 u;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                 : "l"(p)
+                 : "memory");
+    Storage<T>::unpack(u, v);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
+    st_stream32(p, w);
+  } else {
+    store_grads<T, 8>(p, v);
+  }
+}
+// Weights: read by every row, so they stay in L1.
+template <typename T>
+__device__ __forceinline__ void load_weights8(const void *w, int w_f32, long long c, float (&v)[8]) {
+  if (sizeof(T) == 4 || w_f32) {
+    const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(w) + c);
+    const float4 a = __ldg(q), b = __ldg(q + 1);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  } else if constexpr (sizeof(T) == 2) {
+    Storage<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(w) + c)), v);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float load_weight(const void *w, int w_f32, long long c) {
+  return sizeof(T) == 4 || w_f32 ? static_cast<const float *>(w)[c] : Storage<T>::widen(static_cast<const T *>(w)[c]);
+}
+
+__device__ __forceinline__ uint32_t fp8_pair(float lo, float hi) {
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// The sum over the `tpr` threads (whole warps) of each of the block's rows; `part`: 32 floats that no earlier sum is read
+// from any more.  Every thread of the block takes part.
+__device__ __forceinline__ float row_sum(float v, int tpr, float *part) {
+  v = warp_sum(v);
+  if (tpr == 32) return v;
+  const int warp = threadIdx.x >> 5, warps = tpr >> 5, first = warp / warps * warps;
+  if ((threadIdx.x & 31) == 0) part[warp] = v;
+  __syncthreads();
+  float s = 0.f;
+  for (int i = 0; i < warps; ++i) s += part[first + i];
+  return s;
+}
+
+// ---- rows in vectors ---------------------------------------------------------------------------------------------------
+
+template <typename T, typename TOut, int kPer>
+__global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const Params p, const int tpr) {
+  __shared__ float part[32];
+  const int lane_of_row = threadIdx.x % tpr;
+  const long long t = (long long)blockIdx.x * (blockDim.x / tpr) + threadIdx.x / tpr;
+  const bool live = t < p.T;
+  float h[kPer][kVec], w[kPer][kVec];
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
+    if (live && c < p.H) {
+      load8(static_cast<const T *>(p.x) + t * p.ld_x + c, h[i]);
+      if (p.r) {
+        float r[kVec];
+        load8(static_cast<const T *>(p.r) + t * p.ld_r + c, r);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) h[i][j] += r[j];
+      }
+      load_weights8<T>(p.w, p.w_f32, c, w[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) h[i][j] = w[i][j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) sum = fmaf(h[i][j], h[i][j], sum);
+  const float s = 1.f / sqrtf(fmaf(row_sum(sum, tpr, part), p.inv_h, p.eps));
+  if (live && lane_of_row == 0 && p.rstd) p.rstd[t] = s;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
+    const bool here = live && c < p.H;
+    if (p.r_out && here) store8(static_cast<T *>(p.r_out) + t * p.ld_r_out + c, h[i]);
+    float y[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) y[j] = h[i][j] * s * w[i][j];
+    if constexpr (sizeof(TOut) == 1) {
+      // sixteen neighbouring lanes hold a block of 128 columns
+      float a = kLeastAmax;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) a = fmaxf(a, fabsf(y[j]));
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+      const float scale = a / kFp8Max, inv = 1.f / scale;
+      if (here) {
+        if ((threadIdx.x & 15) == 0) p.scale[t * p.ld_scale + c / kBlockCols] = scale;
+        uint2 q;
+        q.x = fp8_pair(y[0] * inv, y[1] * inv) | fp8_pair(y[2] * inv, y[3] * inv) << 16;
+        q.y = fp8_pair(y[4] * inv, y[5] * inv) | fp8_pair(y[6] * inv, y[7] * inv) << 16;
+        st_stream8(static_cast<uint8_t *>(p.out) + t * p.ld_out + c, q);
+      }
+    } else if (here) {
+      store8(static_cast<TOut *>(p.out) + t * p.ld_out + c, y);
+    }
+  }
+}
+
+// ---- rows of any layout ------------------------------------------------------------------------------------------------
+
+constexpr int kAnyThreads = 256;
+
+__device__ __forceinline__ float block_sum(float v, float *part) {
+  v = warp_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kAnyThreads / 32; ++i) s += part[i];
+  return s;
+}
+
+// A warp takes whole blocks of 128 columns, four a lane, in both sweeps alike: what takes an input's place is written by the
+// thread that has read it last.
+template <typename T, typename TOut>
+__global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params p) {
+  __shared__ float part[kAnyThreads / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long blocks = (p.H + kBlockCols - 1) / kBlockCols;
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
+    const T *x = static_cast<const T *>(p.x) + t * p.ld_x;
+    const T *r = p.r ? static_cast<const T *>(p.r) + t * p.ld_r : nullptr;
+    const auto entry = [&](long long c) { return Storage<T>::widen(x[c]) + (r ? Storage<T>::widen(r[c]) : 0.f); };
+    float sum = 0.f;
+    for (long long b = warp; b < blocks; b += kAnyThreads / 32)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const long long c = b * kBlockCols + j * 32 + lane;
+        const float v = c < p.H ? entry(c) : 0.f;
+        sum = fmaf(v, v, sum);
+      }
+    const float s = 1.f / sqrtf(fmaf(block_sum(sum, part), p.inv_h, p.eps));
+    if (threadIdx.x == 0 && p.rstd) p.rstd[t] = s;
+    for (long long b = warp; b < blocks; b += kAnyThreads / 32) {
+      float h[4], y[4], a = kLeastAmax;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const long long c = b * kBlockCols + j * 32 + lane;
+        h[j] = y[j] = 0.f;
+        if (c < p.H) {
+          h[j] = entry(c);
+          y[j] = h[j] * s * load_weight<T>(p.w, p.w_f32, c);
+        }
+        a = fmaxf(a, fabsf(y[j]));
+      }
+      float scale = 1.f, inv = 1.f;
+      if constexpr (sizeof(TOut) == 1) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+        scale = a / kFp8Max, inv = 1.f / scale;
+        if (lane == 0) p.scale[t * p.ld_scale + b] = scale;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const long long c = b * kBlockCols + j * 32 + lane;
+        if (c >= p.H) continue;
+        if (p.r_out) static_cast<T *>(p.r_out)[t * p.ld_r_out + c] = Storage<T>::narrow(h[j]);
+        if constexpr (sizeof(TOut) == 1)
+          static_cast<uint8_t *>(p.out)[t * p.ld_out + c] = (uint8_t)__nv_cvt_float_to_fp8(y[j] * inv, __NV_SATFINITE, __NV_E4M3);
+        else
+          static_cast<TOut *>(p.out)[t * p.ld_out + c] = Storage<TOut>::narrow(y[j]);
+      }
+    }
+  }
+}
+
+// ---- backward ----------------------------------------------------------------------------------------------------------
+
+struct BackParams {
+  const void *dy, *h, *w, *dr;
+  const float *rstd;
+  void *dx;
+  float *partial;  // [gridDim.x, H]: the blocks' sums of dy h s; NULL without d_weight
+  long long T, H, ld_dy, ld_h, ld_dr, ld_dx;
+  float inv_h;
+  int w_f32;
+};
+
+// A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: its threads keep their columns, and with them the sums of dw.
+template <typename T, typename TD, int kPer>
+__global__ void __launch_bounds__(512, 1) rms_norm_backward_kernel(const BackParams p, const int tpr) {
+  __shared__ float part[2][32];
+  const int lane_of_row = threadIdx.x % tpr, rpb = blockDim.x / tpr, row_of_block = threadIdx.x / tpr;
+  float w[kPer][kVec], dw[kPer][kVec];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) w[i][j] = dw[i][j] = 0.f;
+    if (c < p.H) load_weights8<T>(p.w, p.w_f32, c, w[i]);
+  }
+  int turn = 0;
+  for (long long t0 = (long long)blockIdx.x * rpb; t0 < p.T; t0 += (long long)gridDim.x * rpb, turn ^= 1) {
+    const long long t = t0 + row_of_block;
+    const bool live = t < p.T;
+    const float s = live ? p.rstd[t] : 0.f;
+    float h[kPer][kVec], d[kPer][kVec], r[kPer][kVec];
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
+      if (live && c < p.H) {
+        load8(static_cast<const TD *>(p.dy) + t * p.ld_dy + c, d[i]);
+        load8(static_cast<const T *>(p.h) + t * p.ld_h + c, h[i]);
+        if (p.dr) load8(static_cast<const T *>(p.dr) + t * p.ld_dr + c, r[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) d[i][j] = h[i][j] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        dw[i][j] = fmaf(d[i][j] * s, h[i][j], dw[i][j]);
+        d[i][j] *= w[i][j];
+        dot = fmaf(d[i][j], h[i][j], dot);
+      }
+    dot = row_sum(dot, tpr, part[turn]);  // two sets: one is read while the next row's is written
+    const float k = dot * p.inv_h * s * s;
+    if (p.dx && live) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
+        if (c >= p.H) continue;
+        float o[kVec];
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) o[j] = s * fmaf(-k, h[i][j], d[i][j]) + (p.dr ? r[i][j] : 0.f);
+        store8(static_cast<T *>(p.dx) + t * p.ld_dx + c, o);
+      }
+    }
+  }
+  if (!p.partial) return;
+  // the rows that a block works on side by side have a row of partial sums each
+  float *to = p.partial + ((long long)blockIdx.x * rpb + row_of_block) * p.H;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
+    if (c < p.H)
+#pragma unroll
+      for (int j = 0; j < kVec; j += 4)
+        *reinterpret_cast<float4 *>(to + c + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
+  }
+}
+
+template <typename T, typename TD>
+__global__ void __launch_bounds__(kAnyThreads) rms_norm_backward_any_kernel(const BackParams p) {
+  __shared__ float part[kAnyThreads / 32];
+  float *to = p.partial ? p.partial + (long long)blockIdx.x * p.H : nullptr;
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
+    const TD *dy = static_cast<const TD *>(p.dy) + t * p.ld_dy;
+    const T *h = static_cast<const T *>(p.h) + t * p.ld_h;
+    const float s = p.rstd[t];
+    float dot = 0.f;
+    for (long long c = threadIdx.x; c < p.H; c += kAnyThreads)
+      dot = fmaf(Storage<TD>::widen(dy[c]) * load_weight<T>(p.w, p.w_f32, c), Storage<T>::widen(h[c]), dot);
+    const float k = block_sum(dot, part) * p.inv_h * s * s;
+    for (long long c = threadIdx.x; c < p.H; c += kAnyThreads) {
+      const float d = Storage<TD>::widen(dy[c]), hc = Storage<T>::widen(h[c]);
+      // a thread has the same columns in every row: it adds to what it has written itself
+      if (to) to[c] = fmaf(d * s, hc, t == blockIdx.x ? 0.f : to[c]);
+      if (!p.dx) continue;
+      float o = s * fmaf(-k, hc, d * load_weight<T>(p.w, p.w_f32, c));
+      if (p.dr) o += Storage<T>::widen(static_cast<const T *>(p.dr)[t * p.ld_dr + c]);
+      static_cast<T *>(p.dx)[t * p.ld_dx + c] = Storage<T>::narrow(o);
+    }
+  }
+}
+
+// dw (+)= the sum of the partial rows: 32 columns a block, eight threads a column, in a fixed order.
+__global__ void __launch_bounds__(256) sum_partials_kernel(const float *partial, int rows, long long H, float *dw,
+                                                           int accumulate) {
+  __shared__ float part[8][33];
+  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * 32 + col;
+  float v = 0.f;
+  if (c < H)
+    for (int r = slice; r < rows; r += 8) v += partial[(long long)r * H + c];
+  part[slice][col] = v;
+  __syncthreads();
+  if (slice == 0 && c < H) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += part[i][col];
+    dw[c] = accumulate ? dw[c] + v : v;
+  }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------
+
+inline bool dtype_ok(int d) { return d == DVP_F32 || d == DVP_BF16 || d == DVP_F16; }
+inline long long size_of(int d) { return d == DVP_F32 ? 4 : d == DVP_E4M3 ? 1 : 2; }
+// Rows of vectors: every row begins on the boundary of eight elements.
+inline bool vectors(const void *base, long long ld, int dtype) {
+  return !base || ((uintptr_t)base % (8 * size_of(dtype)) == 0 && ld % kVec == 0);
+}
+// float32 weights are read in 16 bytes.
+inline bool weight_vectors(const void *w) { return (uintptr_t)w % 16 == 0; }
+
+struct Shape {
+  int per, tpr, rpb;  // vectors a thread, threads a row, rows a block
+};
+// Two vectors a thread where the row has enough of them, so that a row of 4,096 is eight warps with 32 bytes a thread and
+// matrix in flight.  per = 0: too long for the registers, or no vector at all.
+inline Shape shape_of(long long H, bool backward) {
+  const long long nv = H / kVec;
+  const int per = nv < 1 ? 0 : nv <= 64 ? 1 : nv <= (backward ? 1024 : 2048) ? 2 : backward && nv <= 2048 ? 4 : 0;
+  if (!per) return {0, 0, 0};
+  const int tpr = (int)(((nv + per - 1) / per + 31) / 32 * 32);
+  return {per, tpr, tpr >= 256 ? 1 : 256 / tpr};
+}
+
+// Calls f with a value of the storage type that `d` names.
+template <typename F>
+cudaError_t by_type(int d, F f) {
+  if (d == DVP_F32) return f(float());
+  if (d == DVP_BF16) return f(__nv_bfloat16());
+  return f(__half());
+}
+
+template <typename T, typename TOut>
+cudaError_t launch_forward(const Params &p, bool fast, cudaStream_t stream) {
+  const Shape sh = shape_of(p.H, false);
+  if (fast && sh.per) {
+    const unsigned grid = (unsigned)((p.T + sh.rpb - 1) / sh.rpb), block = (unsigned)(sh.tpr * sh.rpb);
+    if (sh.per == 1)
+      rms_norm_kernel<T, TOut, 1><<<grid, block, 0, stream>>>(p, sh.tpr);
+    else
+      rms_norm_kernel<T, TOut, 2><<<grid, block, 0, stream>>>(p, sh.tpr);
+  } else {
+    rms_norm_any_kernel<T, TOut><<<(unsigned)p.T, kAnyThreads, 0, stream>>>(p);
+  }
+  return cudaGetLastError();
+}
+
+// Blocks of the backward kernel: what the chip holds at once, no more than there are rows.
+inline int backward_blocks(long long T, int rpb) {
+  const long long want = (T + rpb - 1) / rpb, most = kMaxPartials / rpb;
+  return (int)(want < most ? want : most);
+}
+
+template <typename T, typename TD>
+cudaError_t launch_backward(const BackParams &p, bool fast, float *dw, int accumulate, cudaStream_t stream) {
+  const Shape sh = shape_of(p.H, true);
+  int rows;
+  if (fast && sh.per) {
+    const int grid = backward_blocks(p.T, sh.rpb), block = sh.tpr * sh.rpb;
+    rows = grid * sh.rpb;
+    if (sh.per == 1)
+      rms_norm_backward_kernel<T, TD, 1><<<grid, block, 0, stream>>>(p, sh.tpr);
+    else if (sh.per == 2)
+      rms_norm_backward_kernel<T, TD, 2><<<grid, block, 0, stream>>>(p, sh.tpr);
+    else
+      rms_norm_backward_kernel<T, TD, 4><<<grid, block, 0, stream>>>(p, sh.tpr);
+  } else {
+    rows = backward_blocks(p.T, 1);
+    rms_norm_backward_any_kernel<T, TD><<<rows, kAnyThreads, 0, stream>>>(p);
+  }
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || !dw) return e;
+  sum_partials_kernel<<<(unsigned)((p.H + 31) / 32), 256, 0, stream>>>(p.partial, rows, p.H, dw, accumulate);
+  return cudaGetLastError();
+}
+
+// Whatever layout the pointers turn out to have: the most partial rows of both kinds of kernel.
+size_t backward_workspace(const dvp_rms_norm_backward_args *a) {
+  if (!a || a->struct_size != sizeof(*a) || a->T < 0 || a->H < 1 || !a->d_weight) return 0;
+  return (size_t)(a->T < kMaxPartials ? (a->T + 7) / 8 * 8 : kMaxPartials) * (size_t)a->H * sizeof(float);
+}
+
+constexpr long long kMost = 0x7fffff00LL;
+
+}  // namespace norm
+
+size_t rms_norm_backward_workspace(const void *args) {
+  return norm::backward_workspace(static_cast<const dvp_rms_norm_backward_args *>(args));
+}
+
+}  // namespace dvp
+
+extern "C" {
+
+int dvp_rms_norm(const dvp_rms_norm_args *a) {
+  using namespace dvp;
+  using namespace dvp::norm;
+  if (!a || a->struct_size != sizeof(dvp_rms_norm_args)) return DVP_ERR_INVALID_ARG;
+  if (!dtype_ok(a->x_dtype) || (a->weight_dtype != a->x_dtype && a->weight_dtype != DVP_F32)) return DVP_ERR_UNSUPPORTED;
+  const bool fp8 = a->out_dtype == DVP_E4M3;
+  if (!fp8 && !dtype_ok(a->out_dtype)) return DVP_ERR_UNSUPPORTED;
+  if (a->T < 0 || a->H < 1 || !(a->eps >= 0.0 && std::isfinite(a->eps))) return DVP_ERR_INVALID_ARG;
+  if (a->T > kMost || a->H > kMost) return DVP_ERR_UNSUPPORTED;
+  if ((a->scale != nullptr) != fp8 && a->T > 0) return DVP_ERR_INVALID_ARG;
+  if (a->T == 0) return DVP_OK;
+  if (!a->x || !a->weight || !a->out || a->ld_x < a->H || a->ld_out < a->H) return DVP_ERR_INVALID_ARG;
+  if ((a->residual && a->ld_residual < a->H) || (a->residual_out && a->ld_residual_out < a->H)) return DVP_ERR_INVALID_ARG;
+  if (fp8 && a->ld_scale < (a->H + kBlockCols - 1) / kBlockCols) return DVP_ERR_INVALID_ARG;
+  Params p{a->x, a->residual, a->weight, a->residual_out, a->out, a->scale, a->rstd, a->T, a->H, a->ld_x, a->ld_residual,
+           a->ld_residual_out, a->ld_out, a->ld_scale, (float)(1.0 / (double)a->H), (float)a->eps, a->weight_dtype == DVP_F32};
+  const bool fast = a->H % kVec == 0 && vectors(a->x, a->ld_x, a->x_dtype) && vectors(a->residual, a->ld_residual, a->x_dtype) &&
+                    vectors(a->residual_out, a->ld_residual_out, a->x_dtype) && vectors(a->out, a->ld_out, a->out_dtype) &&
+                    weight_vectors(a->weight);
+  const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+  const cudaError_t e = by_type(a->x_dtype, [&](auto x) {
+    using T = decltype(x);
+    if (fp8) return launch_forward<T, uint8_t>(p, fast, stream);
+    return by_type(a->out_dtype, [&](auto o) { return launch_forward<T, decltype(o)>(p, fast, stream); });
+  });
+  return e == cudaSuccess ? DVP_OK : DVP_ERR_CUDA;
+}
+
+int dvp_rms_norm_backward(const dvp_rms_norm_backward_args *a) {
+  using namespace dvp;
+  using namespace dvp::norm;
+  if (!a || a->struct_size != sizeof(dvp_rms_norm_backward_args)) return DVP_ERR_INVALID_ARG;
+  if (!dtype_ok(a->h_dtype) || !dtype_ok(a->dy_dtype) || (a->weight_dtype != a->h_dtype && a->weight_dtype != DVP_F32))
+    return DVP_ERR_UNSUPPORTED;
+  if (a->T < 0 || a->H < 1) return DVP_ERR_INVALID_ARG;
+  if (a->T > kMost || a->H > kMost) return DVP_ERR_UNSUPPORTED;
+  const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+  if (a->T == 0) {
+    if (!a->d_weight || a->accumulate_dw) return DVP_OK;
+    return cudaMemsetAsync(a->d_weight, 0, (size_t)a->H * sizeof(float), stream) == cudaSuccess ? DVP_OK : DVP_ERR_CUDA;
+  }
+  if (!a->dy || !a->h || !a->weight || !a->rstd || (!a->d_x && !a->d_weight)) return DVP_ERR_INVALID_ARG;
+  if (a->ld_dy < a->H || a->ld_h < a->H || (a->d_residual && a->ld_d_residual < a->H) || (a->d_x && a->ld_d_x < a->H))
+    return DVP_ERR_INVALID_ARG;
+  if (a->d_weight && (!a->workspace || (uintptr_t)a->workspace % 256 || a->workspace_bytes < backward_workspace(a)))
+    return DVP_ERR_WORKSPACE;
+  BackParams p{a->dy, a->h, a->weight, a->d_x ? a->d_residual : nullptr, a->rstd, a->d_x,
+               a->d_weight ? static_cast<float *>(a->workspace) : nullptr, a->T, a->H, a->ld_dy, a->ld_h, a->ld_d_residual,
+               a->ld_d_x, (float)(1.0 / (double)a->H), a->weight_dtype == DVP_F32};
+  const bool fast = a->H % kVec == 0 && vectors(a->dy, a->ld_dy, a->dy_dtype) && vectors(a->h, a->ld_h, a->h_dtype) &&
+                    vectors(a->d_residual, a->ld_d_residual, a->h_dtype) && vectors(a->d_x, a->ld_d_x, a->h_dtype) &&
+                    weight_vectors(a->weight);
+  const cudaError_t e = by_type(a->h_dtype, [&](auto h) {
+    return by_type(a->dy_dtype, [&](auto d) {
+      return launch_backward<decltype(h), decltype(d)>(p, fast, a->d_weight, a->accumulate_dw, stream);
+    });
+  });
+  return e == cudaSuccess ? DVP_OK : DVP_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,99 @@
+"""The entry points of the rollout's last stage without a GPU: struct layouts, and argument errors before any CUDA call."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2512_23087_b200 import build, binding
+    build.build()
+    return binding.load_library()
+
+
+def _structs():
+    from paper_2512_23087_b200 import binding as b
+    return {"dvp_rms_norm_args": b.RmsNormArgs, "dvp_rms_norm_backward_args": b.RmsNormBackwardArgs}
+
+
+def test_struct_layout_matches_the_header(tmp_path):
+    structs = _structs()
+    lines = []
+    for cname, cls in structs.items():
+        lines.append(f'printf("{cname} %zu\\n", sizeof({cname}));')
+        lines += [f'printf("{cname}.{f[0]} %zu\\n", offsetof({cname}, {f[0]}));' for f in cls._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "dvp.h"\nint main(void){' + "".join(lines) + "return 0;}\n")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    out = dict(l.split() for l in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines())
+    for cname, cls in structs.items():
+        assert int(out[cname]) == ctypes.sizeof(cls), cname
+        for f in cls._fields_:
+            assert int(out[f"{cname}.{f[0]}"]) == getattr(cls, f[0]).offset, f"{cname}.{f[0]}"
+
+
+def _filled(cls, **fields):
+    a = cls()
+    a.struct_size = ctypes.sizeof(cls)
+    for name, value in fields.items():
+        setattr(a, name, value)
+    return a
+
+
+def _refused(fn, cls, good, cases):
+    """Every case differs from `good`, which would be launched, in what makes it wrong."""
+    for status, change in cases:
+        assert fn(ctypes.byref(_filled(cls, **{**good, **change}))) == status, change
+
+
+def test_norm_refusals(lib):
+    from paper_2512_23087_b200 import binding as b
+    bad, unsupported = b.DVP_ERR_INVALID_ARG, b.DVP_ERR_UNSUPPORTED
+    fn = ctypes.CDLL(b.LIB_PATH).dvp_rms_norm
+    good = dict(x_dtype=b.DVP_BF16, weight_dtype=b.DVP_BF16, out_dtype=b.DVP_E4M3, T=4, H=300, ld_x=300, ld_residual=300,
+                ld_residual_out=300, ld_out=300, ld_scale=3, eps=1e-6, x=0x1000, residual=0x2000, weight=0x3000,
+                residual_out=0x4000, out=0x5000, scale=0x6000, rstd=0x7000)
+    assert fn(None) == bad
+    _refused(fn, b.RmsNormArgs, good, [
+        (bad, dict(struct_size=8)), (bad, dict(T=-1)), (bad, dict(H=0)), (bad, dict(eps=-1.0)), (bad, dict(eps=float("nan"))),
+        (bad, dict(eps=float("inf"))), (bad, dict(x=None)), (bad, dict(weight=None)), (bad, dict(out=None)), (bad, dict(scale=None)),
+        (bad, dict(out_dtype=b.DVP_BF16)), (bad, dict(ld_x=299)), (bad, dict(ld_residual=299)), (bad, dict(ld_residual_out=299)),
+        (bad, dict(ld_out=299)), (bad, dict(ld_scale=2)), (unsupported, dict(x_dtype=b.DVP_E4M3)), (unsupported, dict(x_dtype=9)),
+        (unsupported, dict(weight_dtype=b.DVP_F16)), (unsupported, dict(out_dtype=4)), (unsupported, dict(T=1 << 31)),
+        (b.DVP_OK, dict(T=0))])
+
+
+def test_norm_backward_refusals(lib):
+    from paper_2512_23087_b200 import binding as b
+    bad, unsupported = b.DVP_ERR_INVALID_ARG, b.DVP_ERR_UNSUPPORTED
+    fn = ctypes.CDLL(b.LIB_PATH).dvp_rms_norm_backward
+    good = dict(h_dtype=b.DVP_BF16, weight_dtype=b.DVP_F32, dy_dtype=b.DVP_F32, T=4, H=300, ld_dy=300, ld_h=300, ld_d_residual=300,
+                ld_d_x=300, dy=0x1000, h=0x2000, weight=0x3000, rstd=0x4000, d_residual=0x5000, d_x=0x6000, d_weight=0x7000,
+                workspace=0x8000, workspace_bytes=1 << 30)
+    need = lib.dvp_workspace_bytes(b.DVP_ENTRY_RMS_NORM_BACKWARD, ctypes.byref(_filled(b.RmsNormBackwardArgs, **good)))
+    assert 4 * 300 * 4 <= need < 1 << 20
+    _refused(fn, b.RmsNormBackwardArgs, good, [
+        (bad, dict(struct_size=8)), (bad, dict(T=-1)), (bad, dict(H=0)), (bad, dict(dy=None)), (bad, dict(h=None)),
+        (bad, dict(weight=None)), (bad, dict(rstd=None)), (bad, dict(d_x=None, d_weight=None)), (bad, dict(ld_dy=299)),
+        (bad, dict(ld_h=299)), (bad, dict(ld_d_residual=299)), (bad, dict(ld_d_x=299)), (unsupported, dict(h_dtype=b.DVP_E4M3)),
+        (unsupported, dict(dy_dtype=5)), (unsupported, dict(weight_dtype=b.DVP_F16)), (unsupported, dict(H=1 << 31)),
+        (b.DVP_ERR_WORKSPACE, dict(workspace=None)), (b.DVP_ERR_WORKSPACE, dict(workspace=0x8010)),
+        (b.DVP_ERR_WORKSPACE, dict(workspace_bytes=need - 1)), (b.DVP_OK, dict(T=0, accumulate_dw=1))])
+
+
+@pytest.mark.parametrize("T,H", [(1, 1), (7, 64), (591, 96), (592, 96), (593, 64), (100000, 4096), (3, 20011)])
+def test_norm_backward_workspace_holds_every_partial_row(lib, T, H):
+    """Blocks of up to eight rows side by side, 592 rows of partial sums at most."""
+    from paper_2512_23087_b200 import binding as b
+    a = _filled(b.RmsNormBackwardArgs, T=T, H=H, d_weight=0x1000)
+    need = lib.dvp_workspace_bytes(b.DVP_ENTRY_RMS_NORM_BACKWARD, ctypes.byref(a))
+    for rpb in (1, 2, 4, 8):
+        blocks = min(-(-T // rpb), 592 // rpb)
+        assert need >= blocks * rpb * H * 4
+    a.d_weight = None
+    assert lib.dvp_workspace_bytes(b.DVP_ENTRY_RMS_NORM_BACKWARD, ctypes.byref(a)) == 0
