@@ -592,6 +592,60 @@ typedef struct {
 int dvp_rms_norm_backward(const dvp_rms_norm_backward_args *args);
 
 /*
+ * dvp_quantize_fp8 -- a matrix in 8 bits: q = e4m3(x / c) with c = max(max |x|, 2^-96) / 448 over blocks of `block_rows` x 128.
+ *   x           device [rows, ld_x] of x_dtype (DVP_F32, DVP_BF16, DVP_F16)
+ *   out         device [rows, ld_out] bytes; for dvp_gemm_fp8 ld_out is a multiple of 16
+ *   scale       device [ceil(rows / block_rows), ld_scale] float32, ld_scale >= ceil(cols / 128)
+ *   block_rows  128 (weights) or 1 (activations)
+ * Values that are not finite as in dvp_rms_norm.  Errors: DVP_ERR_INVALID_ARG, DVP_ERR_UNSUPPORTED as there.
+ */
+typedef struct {
+  uint32_t struct_size;
+  int32_t x_dtype;
+  int64_t rows, cols;
+  int64_t ld_x, ld_out, ld_scale;
+  const void *x;
+  void *out;
+  float *scale;
+  void *stream;
+  int32_t block_rows;
+  uint32_t reserved_;
+} dvp_quantize_fp8_args;
+
+int dvp_quantize_fp8(const dvp_quantize_fp8_args *args);
+
+/*
+ * dvp_gemm_fp8 -- the LM head in 8 bits: with blocks k(j) of 128 columns,
+ *   C[m, n] = sum_j a_scale[m, j] b_scale[n / 128, j] sum_{k in k(j)} A[m, k] B[n, k]
+ * The inner sums are formed by the tensor cores, the outer one in float32 registers, and C is rounded once.
+ *
+ *   a        device [M, lda] e4m3 (hidden rows), a_scale device [M, ld_a_scale] float32, ld_a_scale >= ceil(K / 128)
+ *   b        device [N, ldb] e4m3 (LM-head rows), b_scale device [ceil(N / 128), ld_b_scale] float32
+ *   c        device [M, ldc] of c_dtype (DVP_F32, DVP_BF16, DVP_F16), any stride and alignment to its element
+ *   status   device int32: 0 after a run in which every kernel finished, non-zero if one gave up waiting (C is then invalid)
+ *   launch_hint  0 = library default; 1: the kernel of 256 x 256 tiles; 2: the one for few tokens, M <= 128.  Tuning only:
+ *            results differ in the order of the sums alone
+ * a and b on 16-byte boundaries, lda and ldb multiples of 16 (DVP_ERR_UNSUPPORTED otherwise); K itself may be any.  Needs no
+ * workspace.  M = 0 or N = 0 is a valid no-op.  Errors: DVP_ERR_INVALID_ARG (null pointers, negative sizes, K < 1, short
+ * strides, launch_hint), DVP_ERR_UNSUPPORTED, DVP_ERR_CUDA.
+ */
+typedef struct {
+  uint32_t struct_size;
+  int32_t c_dtype;
+  int64_t M, N, K;
+  int64_t lda, ldb, ldc, ld_a_scale, ld_b_scale;
+  const void *a, *b;
+  const float *a_scale, *b_scale;
+  void *c;
+  int32_t *status;
+  void *stream;
+  uint32_t launch_hint;
+  uint32_t reserved_;
+} dvp_gemm_fp8_args;
+
+int dvp_gemm_fp8(const dvp_gemm_fp8_args *args);
+
+/*
  * Bytes of device workspace the entry point needs for `args` (a pointer to
  * that entry point's args struct; only sizes and dtypes are read).  Returns 0
  * for entry points that need none and for invalid arguments.

@@ -31,7 +31,8 @@ DVP_WEIGHT_NONE, DVP_WEIGHT_RATIO, DVP_WEIGHT_TRUNCATE, DVP_WEIGHT_MASK = 0, 1, 
 EXPORTS = ("dvp_forward", "dvp_backward", "dvp_fused_lmhead_forward_backward",
            "dvp_fused_lmhead_forward_backward_static", "dvp_sequence_aggregate", "dvp_monitor", "dvp_gemm_tn",
            "dvp_workspace_bytes", "dvp_status_string", "dvp_version", "dvp_row_wait_status",
-           "dvp_static_workspace_status", "dvp_debug_bounds_status", "dvp_rms_norm", "dvp_rms_norm_backward")
+           "dvp_static_workspace_status", "dvp_debug_bounds_status", "dvp_rms_norm", "dvp_rms_norm_backward",
+           "dvp_quantize_fp8", "dvp_gemm_fp8")
 
 _DTYPES = {torch.float32: DVP_F32, torch.bfloat16: DVP_BF16, torch.float16: DVP_F16}
 _OUT_DTYPES = {**_DTYPES, torch.float8_e4m3fn: DVP_E4M3}
@@ -235,6 +236,48 @@ class RmsNormBackwardArgs(ctypes.Structure):
     ]
 
 
+class QuantizeFp8Args(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("x_dtype", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("ld_x", ctypes.c_int64),
+        ("ld_out", ctypes.c_int64),
+        ("ld_scale", ctypes.c_int64),
+        ("x", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+        ("block_rows", ctypes.c_int32),
+        ("reserved_", ctypes.c_uint32),
+    ]
+
+
+class GemmFp8Args(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("c_dtype", ctypes.c_int32),
+        ("M", ctypes.c_int64),
+        ("N", ctypes.c_int64),
+        ("K", ctypes.c_int64),
+        ("lda", ctypes.c_int64),
+        ("ldb", ctypes.c_int64),
+        ("ldc", ctypes.c_int64),
+        ("ld_a_scale", ctypes.c_int64),
+        ("ld_b_scale", ctypes.c_int64),
+        ("a", ctypes.c_void_p),
+        ("b", ctypes.c_void_p),
+        ("a_scale", ctypes.c_void_p),
+        ("b_scale", ctypes.c_void_p),
+        ("c", ctypes.c_void_p),
+        ("status", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+        ("launch_hint", ctypes.c_uint32),
+        ("reserved_", ctypes.c_uint32),
+    ]
+
+
 # The hot entry points are called with their argument structs packed in one go: setting the fields of a ctypes
 # structure one by one costs several microseconds a call.
 _FORWARD_PACK = struct.Struct("=I3i5qd5Q18Q3QIIfIffQ")
@@ -244,6 +287,9 @@ _SEQUENCE_PACK = struct.Struct("=II2q2Qd9Q")
 _FUSED_PACK = struct.Struct("=Ii8qd7Qii18Q5QIff4xQ")
 _RMS_NORM_PACK = struct.Struct("=I3i7qd8Q")
 _RMS_NORM_BACKWARD_PACK = struct.Struct("=I3i6q10QiI")
+_QUANTIZE_FP8_PACK = struct.Struct("=Ii5q4QiI")
+_GEMM_FP8_PACK = struct.Struct("=Ii8q7QII")
+assert _QUANTIZE_FP8_PACK.size == ctypes.sizeof(QuantizeFp8Args) and _GEMM_FP8_PACK.size == ctypes.sizeof(GemmFp8Args)
 assert _RMS_NORM_PACK.size == ctypes.sizeof(RmsNormArgs)
 assert _RMS_NORM_BACKWARD_PACK.size == ctypes.sizeof(RmsNormBackwardArgs)
 assert _FUSED_PACK.size == ctypes.sizeof(FusedArgs)
@@ -301,11 +347,9 @@ def load_library() -> ctypes.CDLL:
         lib.dvp_static_workspace_status.restype = ctypes.c_int
         lib.dvp_debug_bounds_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
         lib.dvp_debug_bounds_status.restype = ctypes.c_int
-        for name in ("dvp_rms_norm", "dvp_rms_norm_backward"):
-            lib[name].restype = ctypes.c_int
         lib.packed = {}   # the entry points that take a packed struct
         for name in ("dvp_forward", "dvp_backward", "dvp_monitor", "dvp_sequence_aggregate", "dvp_rms_norm",
-                     "dvp_rms_norm_backward"):
+                     "dvp_rms_norm_backward", "dvp_quantize_fp8", "dvp_gemm_fp8"):
             fn = lib[name]   # a function object of its own, with its own argtypes
             fn.argtypes, fn.restype = [ctypes.c_char_p], ctypes.c_int
             lib.packed[name] = fn
@@ -824,3 +868,63 @@ def dvp_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tenso
     if st != DVP_OK:
         raise DvpError(st, "dvp_rms_norm_backward")
     return SimpleNamespace(d_x=d_x, d_weight=d_weight)
+
+
+def dvp_quantize_fp8(x: torch.Tensor, *, block_rows: int = FP8_BLOCK, stream=None):
+    """``x`` [rows, cols] in 8 bits with a float32 scale for each block of ``block_rows`` (128: weights, 1: activations) x 128
+    columns: a namespace with ``q`` (float8_e4m3fn, rows on 16-byte boundaries) and ``scale``, which ``dvp_gemm_fp8`` takes.
+    ``q * scale`` stands for ``x``."""
+    packed = load_library().packed
+    _check_matrix("x", x)
+    if x.dtype not in _DTYPES:
+        raise TypeError("x must be float32, bfloat16 or float16")
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError(f"block_rows must be 1 or {FP8_BLOCK}")
+    rows, cols = x.shape
+    q = x.new_empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn)[:, :cols]
+    scale = x.new_empty((-(-rows // block_rows), -(-cols // FP8_BLOCK)), dtype=torch.float32)
+    with _on_device_of(x):
+        st = packed["dvp_quantize_fp8"](_QUANTIZE_FP8_PACK.pack(
+            _QUANTIZE_FP8_PACK.size, _DTYPES[x.dtype], rows, cols, x.stride(0), q.stride(0), scale.stride(0), x.data_ptr(),
+            q.data_ptr(), scale.data_ptr(), _stream(stream), block_rows, 0))
+    if st != DVP_OK:
+        raise DvpError(st, "dvp_quantize_fp8")
+    return SimpleNamespace(q=q, scale=scale)
+
+
+def dvp_gemm_fp8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, *,
+                 out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, stream=None, launch_hint: int = 0):
+    """``(a * a_scale) @ (b * b_scale).T`` on the tensor cores: ``a`` [M, K] and ``b`` [N, K] are float8_e4m3fn with rows on
+    16-byte boundaries, ``a_scale`` [M, ceil(K / 128)] and ``b_scale`` [ceil(N / 128), ceil(K / 128)] their float32 scales
+    (``dvp_rms_norm``, ``dvp_quantize_fp8``).  Sums over a block of 128 are formed in the tensor cores and added up in
+    float32; the result is rounded once, to ``out_dtype``.  Returns (out, status) as ``dvp_gemm_tn`` does."""
+    packed = load_library().packed
+    for name, x, dtype in (("a", a, torch.float8_e4m3fn), ("b", b, torch.float8_e4m3fn), ("a_scale", a_scale, torch.float32),
+                           ("b_scale", b_scale, torch.float32)):
+        _check_matrix(name, x)
+        if x.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}")
+    (M, K), N = a.shape, b.shape[0]
+    if b.shape[1] != K:
+        raise ValueError("a and b must have the same number of columns")
+    blocks = -(-K // FP8_BLOCK)
+    if a_scale.shape != (M, blocks) or b_scale.shape != (-(-N // FP8_BLOCK), blocks):
+        raise ValueError("a_scale must be [M, ceil(K / 128)] and b_scale [ceil(N / 128), ceil(K / 128)]")
+    if out is None:
+        out = a.new_empty((M, N), dtype=out_dtype)
+    else:
+        _check_matrix("out", out)
+        if out.shape != (M, N):
+            raise ValueError(f"out must be {(M, N)}")
+    if out.dtype not in _DTYPES:
+        raise TypeError("out must be float32, bfloat16 or float16")
+    _check_same_device(a, a_scale=a_scale, b=b, b_scale=b_scale, out=out)
+    status = a.new_empty(1, dtype=torch.int32) if M and N else a.new_zeros(1, dtype=torch.int32)
+    with _on_device_of(a):
+        st = packed["dvp_gemm_fp8"](_GEMM_FP8_PACK.pack(
+            _GEMM_FP8_PACK.size, _DTYPES[out.dtype], M, N, K, a.stride(0), b.stride(0), out.stride(0), a_scale.stride(0),
+            b_scale.stride(0), a.data_ptr(), b.data_ptr(), a_scale.data_ptr(), b_scale.data_ptr(), out.data_ptr(),
+            status.data_ptr(), _stream(stream), launch_hint & _UINT32, 0))
+    if st != DVP_OK:
+        raise DvpError(st, "dvp_gemm_fp8")
+    return out, status

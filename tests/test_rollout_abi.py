@@ -17,7 +17,8 @@ def lib():
 
 def _structs():
     from paper_2512_23087_b200 import binding as b
-    return {"dvp_rms_norm_args": b.RmsNormArgs, "dvp_rms_norm_backward_args": b.RmsNormBackwardArgs}
+    return {"dvp_rms_norm_args": b.RmsNormArgs, "dvp_rms_norm_backward_args": b.RmsNormBackwardArgs,
+            "dvp_quantize_fp8_args": b.QuantizeFp8Args, "dvp_gemm_fp8_args": b.GemmFp8Args}
 
 
 def test_struct_layout_matches_the_header(tmp_path):
@@ -97,3 +98,32 @@ def test_norm_backward_workspace_holds_every_partial_row(lib, T, H):
         assert need >= blocks * rpb * H * 4
     a.d_weight = None
     assert lib.dvp_workspace_bytes(b.DVP_ENTRY_RMS_NORM_BACKWARD, ctypes.byref(a)) == 0
+
+
+def test_quantiser_refusals(lib):
+    from paper_2512_23087_b200 import binding as b
+    bad, unsupported = b.DVP_ERR_INVALID_ARG, b.DVP_ERR_UNSUPPORTED
+    fn = ctypes.CDLL(b.LIB_PATH).dvp_quantize_fp8
+    good = dict(x_dtype=b.DVP_F16, rows=5, cols=200, ld_x=200, ld_out=208, ld_scale=2, x=0x1000, out=0x2000, scale=0x3000,
+                block_rows=128)
+    _refused(fn, b.QuantizeFp8Args, good, [
+        (bad, dict(struct_size=0)), (bad, dict(rows=-1)), (bad, dict(cols=0)), (bad, dict(block_rows=64)), (bad, dict(x=None)),
+        (bad, dict(out=None)), (bad, dict(scale=None)), (bad, dict(ld_x=199)), (bad, dict(ld_out=199)), (bad, dict(ld_scale=1)),
+        (unsupported, dict(x_dtype=b.DVP_E4M3)), (unsupported, dict(rows=1 << 31)),
+        (unsupported, dict(rows=1 << 30, cols=1 << 30, ld_x=1 << 30, ld_out=1 << 30, ld_scale=1 << 23)), (b.DVP_OK, dict(rows=0))])
+
+
+def test_product_refusals(lib):
+    from paper_2512_23087_b200 import binding as b
+    bad, unsupported = b.DVP_ERR_INVALID_ARG, b.DVP_ERR_UNSUPPORTED
+    fn = ctypes.CDLL(b.LIB_PATH).dvp_gemm_fp8
+    good = dict(c_dtype=b.DVP_BF16, M=5, N=300, K=200, lda=208, ldb=208, ldc=300, ld_a_scale=2, ld_b_scale=2, a=0x1000, b=0x2000,
+                a_scale=0x3000, b_scale=0x4000, c=0x5000, status=0x6000)
+    _refused(fn, b.GemmFp8Args, good, [
+        (bad, dict(struct_size=0)), (bad, dict(M=-1)), (bad, dict(N=-1)), (bad, dict(K=0)), (bad, dict(launch_hint=3)),
+        (bad, dict(launch_hint=2, M=129)), (bad, dict(a=None)), (bad, dict(b=None)), (bad, dict(a_scale=None)),
+        (bad, dict(b_scale=None)), (bad, dict(c=None)), (bad, dict(status=None)), (bad, dict(lda=192)), (bad, dict(ldb=192)),
+        (bad, dict(ldc=299)), (bad, dict(ld_a_scale=1)), (bad, dict(ld_b_scale=1)), (unsupported, dict(c_dtype=b.DVP_E4M3)),
+        (unsupported, dict(lda=200)), (unsupported, dict(ldb=200)), (unsupported, dict(a=0x1008)), (unsupported, dict(b=0x2004)),
+        (unsupported, dict(N=1 << 31)), (unsupported, dict(M=0x7fffff00, N=0x7fffff00)), (b.DVP_OK, dict(M=0)),
+        (b.DVP_OK, dict(N=0))])
