@@ -646,6 +646,59 @@ typedef struct {
 int dvp_gemm_fp8(const dvp_gemm_fp8_args *args);
 
 /*
+ * dvp_sample -- the rollout's draw: one token per row from the logits of the inference policy, by the min-p safe set (the
+ * policy pi^mp_infer that Thm. 5.3's estimator wants tokens from), top-k, top-p and a temperature.  With m = max_k z_k and
+ * w_k = e^{(z_k - m) / temperature}:
+ *   K0 = { k : z_k > -inf and z_k >= m + temperature ln rho }      Def. 5.1 of softmax(z / temperature)
+ *   K1 = the top_k largest of K0                                   (all of K0 for top_k <= 0)
+ *   K2 = those of K1, in falling order, before which lies less than top_p of the sum of w over K1 (the first always; all of
+ *        K1 for top_p >= 1)
+ * where equal logits stand in the order of their indices, and the token is the first a in K2 with
+ *   sum_{k in K2, k <= a} w_k > uniform * sum_{k in K2} w_k        (the indices' order; the last with w > 0 where none is)
+ * Sums and the decisions that rest on them are formed in double: the token is that of exact arithmetic unless `uniform` lies
+ * within some 1e-12 of a border.  Temperature 0 takes the largest logit (the first of equals): K2 has one token.
+ *
+ *   logits        device [T, ld] of logits_dtype (DVP_F32, DVP_BF16, DVP_F16), any stride and alignment to its element.
+ *                 -inf marks tokens that are not to be drawn
+ *   uniform       device [T] float32 in [0, 1): the random numbers.  What lies outside counts as the nearest of the interval, NaN
+ *                 as 0
+ *   temperature, top_k, top_p, rho   for all rows, or per row where the pointer is not NULL: *_rows device [T] (float32; top_k
+ *                 int32).  temperature is 0 or in [2^-100, 2^100], rho in [0, 1], top_p >= 0.  Of a row's own settings a
+ *                 temperature in (0, 2^-100) counts as 0, a rho or top_p above 1 as 1, one below 0 as 0
+ *   ids           device [T] int64 or int32 (id_dtype): a
+ *   logp          device [T] float32 or NULL: ln softmax(z / temperature)_a   (temperature 0: of temperature 1)
+ *   logp_mp       device [T] float32 or NULL: ln (w_a / sum_{K2} w): with temperature 1, no top_k and top_p 1 the infer.logp_mp
+ *                 of dvp_forward
+ *   count         device [T] int32 or NULL: |K2|
+ *   launch_hint   0 = library default; otherwise the number of blocks that share a row (1, 2, 4 or 8).  Tuning only
+ * A row without a token to draw (all -inf), with a NaN or +inf logit, or with a temperature, rho or top_p that is NaN, or a
+ * temperature that is negative or above 2^100, has a = -1 (which dvp_forward takes as "no sampled token"), NaN log-probabilities
+ * and count 0.  Needs no workspace.  T = 0 is a valid no-op.  Errors: DVP_ERR_INVALID_ARG (null pointers, negative sizes, V < 1,
+ * ld < V, settings for all rows out of range, launch_hint), DVP_ERR_UNSUPPORTED (dtypes, T >= 2^28, V > 2^31 - 2^16).
+ */
+typedef struct {
+  uint32_t struct_size;
+  int32_t logits_dtype;
+  int32_t id_dtype;
+  uint32_t launch_hint;
+  int64_t T, V, ld;
+  const void *logits;
+  const float *uniform;
+  double temperature, top_p, rho;
+  int64_t top_k;
+  const float *temperature_rows;
+  const int32_t *top_k_rows;
+  const float *top_p_rows;
+  const float *rho_rows;
+  void *ids;
+  float *logp, *logp_mp;
+  int32_t *count;
+  void *stream;
+} dvp_sample_args;
+
+int dvp_sample(const dvp_sample_args *args);
+
+/*
  * Bytes of device workspace the entry point needs for `args` (a pointer to
  * that entry point's args struct; only sizes and dtypes are read).  Returns 0
  * for entry points that need none and for invalid arguments.

@@ -32,7 +32,7 @@ EXPORTS = ("dvp_forward", "dvp_backward", "dvp_fused_lmhead_forward_backward",
            "dvp_fused_lmhead_forward_backward_static", "dvp_sequence_aggregate", "dvp_monitor", "dvp_gemm_tn",
            "dvp_workspace_bytes", "dvp_status_string", "dvp_version", "dvp_row_wait_status",
            "dvp_static_workspace_status", "dvp_debug_bounds_status", "dvp_rms_norm", "dvp_rms_norm_backward",
-           "dvp_quantize_fp8", "dvp_gemm_fp8")
+           "dvp_quantize_fp8", "dvp_gemm_fp8", "dvp_sample")
 
 _DTYPES = {torch.float32: DVP_F32, torch.bfloat16: DVP_BF16, torch.float16: DVP_F16}
 _OUT_DTYPES = {**_DTYPES, torch.float8_e4m3fn: DVP_E4M3}
@@ -278,6 +278,33 @@ class GemmFp8Args(ctypes.Structure):
     ]
 
 
+class SampleArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("logits_dtype", ctypes.c_int32),
+        ("id_dtype", ctypes.c_int32),
+        ("launch_hint", ctypes.c_uint32),
+        ("T", ctypes.c_int64),
+        ("V", ctypes.c_int64),
+        ("ld", ctypes.c_int64),
+        ("logits", ctypes.c_void_p),
+        ("uniform", ctypes.c_void_p),
+        ("temperature", ctypes.c_double),
+        ("top_p", ctypes.c_double),
+        ("rho", ctypes.c_double),
+        ("top_k", ctypes.c_int64),
+        ("temperature_rows", ctypes.c_void_p),
+        ("top_k_rows", ctypes.c_void_p),
+        ("top_p_rows", ctypes.c_void_p),
+        ("rho_rows", ctypes.c_void_p),
+        ("ids", ctypes.c_void_p),
+        ("logp", ctypes.c_void_p),
+        ("logp_mp", ctypes.c_void_p),
+        ("count", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
 # The hot entry points are called with their argument structs packed in one go: setting the fields of a ctypes
 # structure one by one costs several microseconds a call.
 _FORWARD_PACK = struct.Struct("=I3i5qd5Q18Q3QIIfIffQ")
@@ -289,6 +316,8 @@ _RMS_NORM_PACK = struct.Struct("=I3i7qd8Q")
 _RMS_NORM_BACKWARD_PACK = struct.Struct("=I3i6q10QiI")
 _QUANTIZE_FP8_PACK = struct.Struct("=Ii5q4QiI")
 _GEMM_FP8_PACK = struct.Struct("=Ii8q7QII")
+_SAMPLE_PACK = struct.Struct("=I2iI3q2Q3dq9Q")
+assert _SAMPLE_PACK.size == ctypes.sizeof(SampleArgs)
 assert _QUANTIZE_FP8_PACK.size == ctypes.sizeof(QuantizeFp8Args) and _GEMM_FP8_PACK.size == ctypes.sizeof(GemmFp8Args)
 assert _RMS_NORM_PACK.size == ctypes.sizeof(RmsNormArgs)
 assert _RMS_NORM_BACKWARD_PACK.size == ctypes.sizeof(RmsNormBackwardArgs)
@@ -349,7 +378,7 @@ def load_library() -> ctypes.CDLL:
         lib.dvp_debug_bounds_status.restype = ctypes.c_int
         lib.packed = {}   # the entry points that take a packed struct
         for name in ("dvp_forward", "dvp_backward", "dvp_monitor", "dvp_sequence_aggregate", "dvp_rms_norm",
-                     "dvp_rms_norm_backward", "dvp_quantize_fp8", "dvp_gemm_fp8"):
+                     "dvp_rms_norm_backward", "dvp_quantize_fp8", "dvp_gemm_fp8", "dvp_sample"):
             fn = lib[name]   # a function object of its own, with its own argtypes
             fn.argtypes, fn.restype = [ctypes.c_char_p], ctypes.c_int
             lib.packed[name] = fn
@@ -928,3 +957,47 @@ def dvp_gemm_fp8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scal
     if st != DVP_OK:
         raise DvpError(st, "dvp_gemm_fp8")
     return out, status
+
+
+def dvp_sample(logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.0, top_k=0, top_p=1.0, rho=0.0,
+               id_dtype: torch.dtype = torch.int64, stream=None, launch_hint: int = 0):
+    """Draws a token per row of the inference ``logits`` [T, V] by the random numbers ``uniform`` [T] in [0, 1): from the min-p
+    safe set of ``softmax(logits / temperature)`` at ``rho`` (Def. 5.1), the ``top_k`` largest of it (0: all), and of these the
+    fewest that hold ``top_p`` of their mass.  Each setting is a number or a tensor of one per row (float32, ``top_k``
+    int32).  Temperature 0 takes the largest logit; equal logits stand in the order of their indices; -inf marks tokens that
+    are not to be drawn.
+
+    Returns a namespace with ``ids`` [T] (-1 for a row that has no token to draw or is not finite), ``logp`` = ln pi(a) at the
+    temperature, ``logp_mp`` = ln of the same renormalised over what is kept (with ``rho`` alone the ``infer.logp_mp`` of
+    ``dvp_forward``) and ``count``, the number of tokens kept."""
+    packed = load_library().packed
+    _check_matrix("logits", logits)
+    T, V = logits.shape
+    if logits.dtype not in _DTYPES:
+        raise TypeError("logits must be float32, bfloat16 or float16")
+    if id_dtype not in (torch.int64, torch.int32):
+        raise TypeError("id_dtype must be int64 or int32")
+    _check_vector("uniform", uniform, T, (torch.float32,))
+    values, rows = [], []
+    for name, v, dtype, none in (("temperature", temperature, torch.float32, 1.0), ("top_k", top_k, torch.int32, 0),
+                                 ("top_p", top_p, torch.float32, 1.0), ("rho", rho, torch.float32, 0.0)):
+        if isinstance(v, torch.Tensor):
+            _check_vector(name, v, T, (dtype,))
+            _check_same_device(logits, **{name: v})
+            values.append(none)
+            rows.append(v.data_ptr() if T else 1)
+        else:
+            values.append(v)
+            rows.append(0)
+    _check_same_device(logits, uniform=uniform)
+    f, at, step = _host.outputs(logits, T, 2, 1)
+    ids = logits.new_empty(T, dtype=id_dtype)
+    with _on_device_of(logits):
+        st = packed["dvp_sample"](_SAMPLE_PACK.pack(
+            _SAMPLE_PACK.size, _DTYPES[logits.dtype], DVP_ID_I64 if id_dtype == torch.int64 else DVP_ID_I32,
+            launch_hint & _UINT32, T, V, logits.stride(0), logits.data_ptr(), uniform.data_ptr(), float(values[0]),
+            float(values[2]), float(values[3]), int(values[1]), *rows, ids.data_ptr(), at, at + step, at + 2 * step,
+            _stream(stream)))
+    if st != DVP_OK:
+        raise DvpError(st, "dvp_sample")
+    return SimpleNamespace(ids=ids, logp=f[0], logp_mp=f[1], count=f[2])

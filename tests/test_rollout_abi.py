@@ -18,7 +18,8 @@ def lib():
 def _structs():
     from paper_2512_23087_b200 import binding as b
     return {"dvp_rms_norm_args": b.RmsNormArgs, "dvp_rms_norm_backward_args": b.RmsNormBackwardArgs,
-            "dvp_quantize_fp8_args": b.QuantizeFp8Args, "dvp_gemm_fp8_args": b.GemmFp8Args}
+            "dvp_quantize_fp8_args": b.QuantizeFp8Args, "dvp_gemm_fp8_args": b.GemmFp8Args,
+            "dvp_sample_args": b.SampleArgs}
 
 
 def test_struct_layout_matches_the_header(tmp_path):
@@ -127,3 +128,19 @@ def test_product_refusals(lib):
         (unsupported, dict(lda=200)), (unsupported, dict(ldb=200)), (unsupported, dict(a=0x1008)), (unsupported, dict(b=0x2004)),
         (unsupported, dict(N=1 << 31)), (unsupported, dict(M=0x7fffff00, N=0x7fffff00)), (b.DVP_OK, dict(M=0)),
         (b.DVP_OK, dict(N=0))])
+
+
+def test_sample_refusals(lib):
+    from paper_2512_23087_b200 import binding as b
+    bad, unsupported, nan = b.DVP_ERR_INVALID_ARG, b.DVP_ERR_UNSUPPORTED, float("nan")
+    fn = ctypes.CDLL(b.LIB_PATH).dvp_sample
+    good = dict(logits_dtype=b.DVP_BF16, id_dtype=b.DVP_ID_I64, T=3, V=100, ld=100, logits=0x1000, uniform=0x2000, temperature=1.0,
+                top_p=0.9, rho=0.1, top_k=5, ids=0x3000, logp=0x4000, logp_mp=0x5000, count=0x6000)
+    _refused(fn, b.SampleArgs, good, [
+        (bad, dict(struct_size=0)), (bad, dict(T=-1)), (bad, dict(V=0)), (bad, dict(ld=99)), (bad, dict(logits=None)),
+        (bad, dict(uniform=None)), (bad, dict(ids=None)), (bad, dict(temperature=-0.5)), (bad, dict(temperature=nan)),
+        (bad, dict(temperature=float("inf"))), (bad, dict(temperature=1e-31)), (bad, dict(temperature=1e31)), (bad, dict(rho=-0.1)),
+        (bad, dict(rho=1.5)), (bad, dict(rho=nan)), (bad, dict(top_p=-0.1)), (bad, dict(top_p=nan)), (bad, dict(launch_hint=3)),
+        (bad, dict(launch_hint=16)), (unsupported, dict(logits_dtype=b.DVP_E4M3)), (unsupported, dict(id_dtype=2)),
+        (unsupported, dict(T=1 << 28)), (unsupported, dict(V=0x7fff0001, ld=0x7fff0001)), (b.DVP_OK, dict(T=0)),
+        (b.DVP_OK, dict(T=0, temperature=nan, temperature_rows=0x7000))])
