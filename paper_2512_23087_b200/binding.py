@@ -1001,3 +1001,20 @@ def dvp_sample(logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.0, 
     if st != DVP_OK:
         raise DvpError(st, "dvp_sample")
     return SimpleNamespace(ids=ids, logp=f[0], logp_mp=f[1], count=f[2])
+
+
+def dvp_rollout_head(x: torch.Tensor, norm_weight: torch.Tensor, w_vocab: torch.Tensor, w_scale: torch.Tensor,
+                     uniform: torch.Tensor, *, residual: torch.Tensor | None = None, eps: float = 1e-6, temperature=1.0, top_k=0,
+                     top_p=1.0, rho=0.0, logits_dtype: torch.dtype = torch.bfloat16, id_dtype: torch.dtype = torch.int64,
+                     stream=None):
+    """The end of a decoding step: the final norm of ``x`` (+ ``residual``) with its result in 8 bits, the LM head in 8 bits
+    (``w_vocab``, ``w_scale`` from ``dvp_quantize_fp8``), and a token per row drawn from its logits; ``dvp_rms_norm``,
+    ``dvp_gemm_fp8`` and ``dvp_sample`` on one stream.
+
+    Returns the namespace of ``dvp_sample`` with ``logits`` [T, V] (the ``infer_logits`` of ``dvp_forward`` and of the fused LM
+    head), ``residual``, ``rstd`` and ``status`` beside it."""
+    n = dvp_rms_norm(x, norm_weight, residual=residual, eps=eps, out_dtype=torch.float8_e4m3fn, stream=stream)
+    logits, status = dvp_gemm_fp8(n.y, n.scale, w_vocab, w_scale, out_dtype=logits_dtype, stream=stream)
+    res = dvp_sample(logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, rho=rho, id_dtype=id_dtype, stream=stream)
+    res.logits, res.residual, res.rstd, res.status = logits, n.residual, n.rstd, status
+    return res
