@@ -26,10 +26,10 @@
 namespace dvp {
 namespace sample {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kList = 2048;
-constexpr int kTable = 64, kCompact = 256;
-constexpr int kSegs = 512;          // sums of pieces in the walk to the token
+constexpr int kTable = 64;
+constexpr int kParts = 128;         // sums that a warp keeps of its part of the row, of one piece or several each
 constexpr int kMostBounds = 32768;  // granules whose maximum is held: 64 KB
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kNoIndex = 0x7fffffff;
@@ -56,23 +56,28 @@ struct Slot {
   int i;
 };
 
+template <typename T>
 struct Shared {
+  static constexpr int kPiece = 32 * 32 / sizeof(T);  // logits of 32 granules
   uint64_t list[kList];
-  uint64_t sorted[kList];
   uint32_t hist[kBins];
   union {
-    float compact[kWarps][kCompact];  // a warp's logits that matter, side by side
-    double seg[kSegs];
+    struct {
+      float value[kWarps][kPiece];  // a warp's logits that matter, side by side
+      uint16_t place[kWarps][kPiece];
+    } compact;
+    uint64_t sorted[kList];
   };
+  double part[kWarps][kParts];  // of the last sum over the row; of the first sweep float32 pairs: a maximum, the sum against it
   double table[kTable];  // 2^(i / kTable)
   double chunk[kWarps];  // the warps' parts of a sum over the row
+  double group[32];      // sums of 32 neighbouring logits
   double warp_a[kWarps], warp_b[kWarps];
   float warp_m[kWarps];
   uint32_t warp_n[kWarps];
   Slot slot[2];
   uint32_t list_n, counter[3];
   uint32_t pick_lo, pick_hi, pick_last;  // of the histogram's bins; the last that holds anything, then what pick_lo to pick_hi hold
-  int unclear;  // whether another cut is possible for a sum that the row can have
 };
 
 // A logit's place in the order as an unsigned number; the zeros are one.
@@ -111,26 +116,78 @@ __device__ __forceinline__ N warp_scan(N v) {
   return v;
 }
 
-// The eight words of a granule as logits.
+struct Words {
+  uint32_t w[8];
+};
+// A granule at the row's ends: what lies outside the row is -inf.
 template <typename T>
-__device__ __forceinline__ void widen(const uint32_t (&w)[8], float (&x)[32 / sizeof(T)]) {
-  Storage<T>::unpack(make_uint4(w[0], w[1], w[2], w[3]), x);
-  Storage<T>::unpack(make_uint4(w[4], w[5], w[6], w[7]), x + 16 / sizeof(T));
+__device__ __noinline__ Words load_end(const T *z, int at, int V) {
+  Words r;
+  const uint16_t *h = reinterpret_cast<const uint16_t *>(z);
+  const uint32_t none = std::is_same<T, __half>::value ? 0xfc00u : 0xff80u;
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      r.w[i] = at + i >= 0 && at + i < V ? __float_as_uint(z[at + i]) : 0xff800000u;
+    } else {
+      const int a = at + 2 * i;
+      r.w[i] = (a >= 0 && a < V ? h[a] : none) | (a + 1 >= 0 && a + 1 < V ? h[a + 1] : none) << 16;
+    }
+  }
+  return r;
+}
+
+// Two float32 in 64 bits, which one instruction adds or multiplies.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ void apart(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+
+// Two neighbouring logits of a granule's eight words.
+template <typename T>
+__device__ __forceinline__ void two_of(const uint32_t (&w)[8], int i, float &lo, float &hi) {
+  if constexpr (sizeof(T) == 4) {
+    lo = __uint_as_float(w[2 * i]), hi = __uint_as_float(w[2 * i + 1]);
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const float2 f = __half22float2(reinterpret_cast<const __half2 &>(w[i]));
+    lo = f.x, hi = f.y;
+  } else {
+    lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
+  }
 }
 
 template <typename T>
 struct Row {
   static constexpr int kPer = 32 / sizeof(T);  // logits of a granule
+  using Shared = sample::Shared<T>;
   Shared *sh;
   uint16_t *bounds;  // bfloat16, rounded up; NULL: none
   const T *z;
   int V, off;                    // off: logits of the first granule that lie in front of the row
   int seg0, segs, all_segs;      // the block's pieces of 32 granules, the row's
   int first, mine;               // of the block's pieces, the warp's
+  int log_q;                     // pieces of a part: 2^log_q
   int blocks, rank, turn;
   int warp, lane;
   double inv_t;
-  float c;  // log2(e) / temperature
+  float c, c_rest;  // log2(e) / temperature, and what float32 leaves of it
   float m;  // the row's maximum
   // what is kept so far
   float cut_v;
@@ -163,25 +220,17 @@ struct Row {
     if (at >= 0 && at + kPer <= V) {
       ld_stream32(z + at, w);
     } else {
-      const uint16_t *h = reinterpret_cast<const uint16_t *>(z);
-      const uint32_t none = std::is_same<T, __half>::value ? 0xfc00u : 0xff80u;
+      const Words r = load_end(z, at, V);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (sizeof(T) == 4) {
-          w[i] = at + i >= 0 && at + i < V ? __float_as_uint(z[at + i]) : 0xff800000u;
-        } else {
-          const int a = at + 2 * i;
-          w[i] = (a >= 0 && a < V ? h[a] : none) | (a + 1 >= 0 && a + 1 < V ? h[a + 1] : none) << 16;
-        }
-      }
+      for (int i = 0; i < 8; ++i) w[i] = r.w[i];
     }
   }
 
   // e^{(x - m) / T} to some 2^-50.  With y = (x - m) / T and k the whole number next to 64 y / ln 2, r = y - k ln 2 / 64 is at most
   // ln 2 / 128, where six terms of the series leave 4e-17; e^y = 2^(k / 64) e^r, the fraction of the power from the table: eleven
   // operations in double.
-  __device__ __forceinline__ double weight(float x) const {
-    const double y = ((double)x - (double)m) * inv_t;
+  __device__ __forceinline__ double weight(float x) const { return power(((double)x - (double)m) * inv_t); }
+  __device__ __forceinline__ double power(double y) const {
     const double big = 6755399441055744.0;  // 1.5 2^52: adding it leaves the whole number in the low bits
     const double shifted = fma(y, 92.33248261689366, big);
     const int k = __double2loint(shifted);
@@ -200,9 +249,18 @@ struct Row {
   // ---- 1: the maximum, the sum beside it, the number of tokens that cannot be drawn
   // Lanes of a warp share the maximum that they have met, so that a larger one, which they turn to together, is rare.  The warps'
   // sums stay in `chunk`, against the row's maximum.
-  __device__ void stats(double &rest, int &masked) {
-    float tm = kNegInf, s = 0.f, n = 0.f;  // the lane's terms: n of e^0, and s
+  struct First {
+    float tm;
+    double s, n;
+    int gone;
+  };
+  __device__ __noinline__ static First first_sweep(const Row row) { return row.sweep_all(); }
+  __device__ __forceinline__ First sweep_all() const {
+    float tm = kNegInf, n = 0.f;  // the lane's terms: n of e^0, and s
+    double s = 0.0;
     int gone = 0;                          // logits of -inf
+    float of_part = 0.f;                   // the part's terms so far
+    double *parts = sh->part[warp];
     constexpr int U = 2;
     uint32_t next[U][8];
 #pragma unroll
@@ -213,9 +271,11 @@ struct Row {
       for (int u = 0; u < U; ++u) {
         if (i0 + u >= mine) break;
         const int seg = first + i0 + u;
-        float x[kPer], hi, lo;
-        widen<T>(next[u], x);
-        extremes(next[u], x, hi, lo);
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = next[u][k];
+        float hi, lo;
+        extremes(w, hi, lo);
         if (i0 + u + U < mine) load(seg + U, next[u]);
         if (bounds) {
           const uint32_t b = __float_as_uint(hi);
@@ -223,38 +283,61 @@ struct Row {
         }
         if (__any_sync(0xffffffffu, lo == kNegInf)) {
 #pragma unroll
-          for (int j = 0; j < kPer; ++j) gone += x[j] == kNegInf;
+          for (int j = 0; j < kPer / 2; ++j) {
+            float a, b;
+            two_of<T>(w, j, a, b);
+            gone += (a == kNegInf) + (b == kNegInf);
+          }
         }
         const float top = warp_max(hi);
-        float g = 0.f;
-        if (top >= tm && top > kNegInf) {
-          if (top > tm) {
-            s = (s + n) * ex2((tm - top) * c);
-            n = 0.f;
-            tm = top;
+        const float ref = fmaxf(fmaxf(tm, top), kLowest);
+        const bool largest = top >= tm && top > kNegInf;
+        if (largest && top > tm) {
+          if (tm > kNegInf) {
+            const double f = power(((double)tm - (double)top) * inv_t);
+            s = (s + (double)n) * f;
+            of_part *= (float)f;
           }
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) {
-            if (x[j] == tm)
-              n += 1.f;
-            else
-              g += ex2((x[j] - tm) * c);
-          }
-        } else {
-          const float ref = fmaxf(tm, kLowest);
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) g += ex2((x[j] - ref) * c);
+          n = 0.f;
+          tm = top;
         }
-        s += g;
+        // terms of the largest are counted; what is -inf, or too far below for the arithmetic, is left out
+        if (largest || __any_sync(0xffffffffu, !((lo - ref) * c > -1e4f))) {
+          unsigned out = 0;
+          float same = 0.f;
+#pragma unroll
+          for (int j = 0; j < kPer / 2; ++j) {
+            float a, b;
+            two_of<T>(w, j, a, b);
+            same += (a == tm ? 1.f : 0.f) + (b == tm ? 1.f : 0.f);
+            out |= (a == ref || (a - ref) * c < -1e4f ? 1u : 0u) << (2 * j) | (b == ref || (b - ref) * c < -1e4f ? 1u : 0u) << (2 * j + 1);
+          }
+          const float g = terms<true>(w, ref, out);
+          s += (double)g;
+          n += same;
+          of_part += g + same;
+        } else {
+          const float g = terms<false>(w, ref, 0);
+          s += (double)g;
+          of_part += g;
+        }
+        const int i = i0 + u;
+        if (((i + 1) & ((1 << log_q) - 1)) == 0 || i + 1 == mine) {
+          of_part = warp_sum(of_part);
+          if (lane == 0) parts[i >> log_q] = __hiloint2double(__float_as_int(tm), __float_as_int(of_part));
+          of_part = 0.f;
+        }
       }
     }
-    const double ws = warp_sum((double)s), wn = warp_sum((double)n);
-    gone = __reduce_add_sync(0xffffffffu, gone);
+    return First{tm, warp_sum(s), warp_sum((double)n), (int)__reduce_add_sync(0xffffffffu, gone)};
+  }
+  __device__ void stats(double &rest, int &masked) {
+    const First f = first_sweep(*this);
     if (lane == 0) {
-      sh->warp_m[warp] = tm;
-      sh->warp_a[warp] = ws;
-      sh->warp_b[warp] = wn;
-      sh->warp_n[warp] = (uint32_t)gone;
+      sh->warp_m[warp] = f.tm;
+      sh->warp_a[warp] = f.s;
+      sh->warp_b[warp] = f.n;
+      sh->warp_n[warp] = (uint32_t)f.gone;
     }
     __syncthreads();
     combine(kWarps, sh->warp_m[lane & (kWarps - 1)], sh->warp_a[lane & (kWarps - 1)], sh->warp_b[lane & (kWarps - 1)], m, rest);
@@ -268,16 +351,17 @@ struct Row {
     masked -= all_segs * 32 * kPer - V;  // what lies outside the row
     if (threadIdx.x < kWarps) {
       const float mi = sh->warp_m[threadIdx.x];
-      sh->chunk[threadIdx.x] = mi > kNegInf ? (sh->warp_a[threadIdx.x] + sh->warp_b[threadIdx.x]) * exp2(((double)mi - (double)m) * (double)c) : 0.0;
+      sh->chunk[threadIdx.x] =
+          mi > kNegInf ? (sh->warp_a[threadIdx.x] + sh->warp_b[threadIdx.x]) * power(((double)mi - (double)m) * inv_t) : 0.0;
     }
     __syncthreads();
   }
   // The largest and the least of a granule; those of 16 bits two at a time.
-  __device__ __forceinline__ static void extremes(const uint32_t (&w)[8], const float (&x)[kPer], float &hi, float &lo) {
+  __device__ __forceinline__ static void extremes(const uint32_t (&w)[8], float &hi, float &lo) {
     if constexpr (sizeof(T) == 4) {
-      hi = x[0], lo = x[0];
+      hi = lo = __uint_as_float(w[0]);
 #pragma unroll
-      for (int j = 1; j < kPer; ++j) hi = fmaxf(hi, x[j]), lo = fminf(lo, x[j]);
+      for (int j = 1; j < kPer; ++j) hi = fmaxf(hi, __uint_as_float(w[j])), lo = fminf(lo, __uint_as_float(w[j]));
     } else {
       using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
       T2 a = reinterpret_cast<const T2 &>(w[0]), b = a;
@@ -301,235 +385,376 @@ struct Row {
       if (top >> lane & 1)
         v = a + (b - (lane == __ffs(top) - 1 ? 1.0 : 0.0));
       else  // nothing or NaN where there is no maximum
-        v = mi > kNegInf ? (a + b) * exp2(((double)mi - (double)mm) * (double)c) : a;
+        v = mi > kNegInf ? (a + b) * power(((double)mi - (double)mm) * inv_t) : a;
     }
     m_out = mm;
     rest = warp_sum(v);
   }
-  // How far the float32 sums of stats() can be off, relative to the whole.  A term 2^a: a passes three roundings of 2^-24 of
-  // itself; terms below 2^-32 of the largest hold 2^-32 V of the whole at most, so |a| counts with less than 33, 33 * 3 ln 2 = 69 times
-  // 2^-24; the exponential 4 times, and a lane's chain of additions of kPer + the granules that it takes, and ten beside it.
-  __device__ __forceinline__ double eps() const { return (double)(90 + kPer + (all_segs / (blocks * kWarps) + 2)) * 5.9604644775390625e-08; }
+  // The sum of 2^{(x - ref) c} over a granule, without the logits in `out`.  The roundings of the product and of c are made good to
+  // first order: 2^{a + r} = 2^a (1 + r ln 2).
+  template <bool kOut>
+  __device__ __forceinline__ float terms(const uint32_t (&w)[8], float ref, unsigned out) const {
+    const uint64_t minus = pair(-ref, -ref), up = pair(c, c), down = pair(-c, -c), rest = pair(c_rest, c_rest);
+    const uint64_t ln2 = pair(0.6931471805599453f, 0.6931471805599453f);
+    uint64_t sum[2];
+#pragma unroll
+    for (int j = 0; j < kPer / 2; ++j) {
+      float lo, hi;
+      two_of<T>(w, j, lo, hi);
+      const uint64_t d = add2(pair(lo, hi), minus), a = mul2(d, down), r = fma2(d, rest, fma2(d, up, a));
+      apart(a, lo, hi);
+      const uint64_t p = pair(ex2(-lo), ex2(-hi));
+      uint64_t e = fma2(p, mul2(r, ln2), p);
+      if constexpr (kOut) {
+        apart(e, lo, hi);
+        e = pair(out >> (2 * j) & 1 ? 0.f : lo, out >> (2 * j + 1) & 1 ? 0.f : hi);
+      }
+      sum[j & 1] = j < 2 ? e : add2(sum[j & 1], e);
+    }
+    float lo, hi;
+    apart(add2(sum[0], sum[1]), lo, hi);
+    return lo + hi;
+  }
+  // How far a sum S of terms() can be off, relative to itself.  With p_k a logit's share of S, its exponent is -log2 p_k - log2 S, and
+  // the mean of these at most the entropy, log2 V, less log2 S.  A difference is rounded once: ln 2 times that mean, times
+  // 2^-24; the exponential is good to 4, what is left of product and c to 1, and a granule's additions take 8 at most.
+  __device__ __forceinline__ double eps(double sum) const {
+    const int bits = 32 - __clz(V) + max(0, 1023 - (int)(__double2hiint(sum) >> 20 & 0x7ff));
+    return (13.0 + 0.6932 * (double)bits) * 5.9604644775390625e-08;
+  }
 
-  // Calls f(x, i0) for the warp's pieces, each lane with its granule (-inf in those that hold nothing from `floor` on).  f is
-  // called by whole warps.
-  template <typename F>
-  __device__ __forceinline__ void sweep(float floor, F f) const {
-    constexpr int U = 2;
-    for (int i0 = 0; i0 < mine; i0 += U) {
-      uint32_t w[U][8];
-      bool any[U];
+  // A bit for each of a granule's logits that is at least v; those of 16 bits are compared two at a time, with the least value of
+  // the type that is.
+  __device__ __forceinline__ static unsigned from(const uint32_t (&w)[8], float v) {
+    unsigned mask = 0;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int seg = first + i0 + u;
-        const bool hot = i0 + u < mine && (!bounds || __uint_as_float((uint32_t)bounds[seg * 32 + lane] << 16) >= floor);
-        any[u] = __any_sync(0xffffffffu, hot);
-        if (hot) {
-          load(seg, w[u]);
-        } else {
+      for (int j = 0; j < kPer; ++j) mask |= __uint_as_float(w[j]) >= v ? 1u << j : 0u;
+    } else {
+      using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+      T2 least;
+      if constexpr (std::is_same<T, __half>::value)
+        least.x = least.y = __float2half_ru(v);
+      else
+        least.x = least.y = __float2bfloat16_ru(v);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[u][i] = std::is_same<T, float>::value ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
+      for (int i = 0; i < 8; ++i) mask |= __hge2_mask(reinterpret_cast<const T2 &>(w[i]), least) & (1u << (2 * i) | 1u << (17 + 2 * i));
+      mask = (mask | mask >> 16) & 0xffff;
+    }
+    return mask;
+  }
+
+  // What a pass over the row looks for: the logits above `v`, those equal to it up to index `i`, none above `most`.  Of these the
+  // ones above `split` are summed up; the others go where `rest` says.
+  enum Rest { kNone, kFirst, kBinsOfKeys, kToList };
+  struct Pass {
+    float v;
+    int i;
+    float most, split;
+    bool weights;  // sums of weights, else of ones
+    Rest rest;
+    uint32_t k_hi;   // kBinsOfKeys
+    int shift;
+  };
+  // What is kept, none below `from`.
+  __device__ __forceinline__ Pass of_kept(float from) const {
+    return Pass{fmaxf(from, cut_v), from > cut_v ? kNoIndex : cut_i, -kNegInf, kNegInf, true, kNone, 0, 0};
+  }
+  struct Sum {
+    double all;  // over the row
+    int n;       // their number; kFirst: the first index
+  };
+  // Reads the granules that can hold such a logit.  A piece's logits that matter are put side by side first: they are few, and
+  // each lane by itself would form exponentials for one or two lanes at a time.  Leaves the warps' sums in `chunk` and tells the
+  // blocks theirs; the order of the additions is fixed.
+  __device__ __noinline__ static Sum pass(Row row, const Pass a) {
+    Shared *sh = row.sh;
+    float *value = sh->compact.value[row.warp];
+    uint16_t *place = sh->compact.place[row.warp];
+    double acc = 0.0, of_part = 0.0;
+    double *parts = sh->part[row.warp];
+    int n = 0, best = kNoIndex;
+    const auto hot = [&](int i) {
+      return i < row.mine &&
+             (!row.bounds || __uint_as_float((uint32_t)row.bounds[(row.first + i) * 32 + row.lane] << 16) >= a.v);
+    };
+    const bool plain = a.i == kNoIndex && a.most == -kNegInf;
+    uint32_t next[8];
+    bool next_hot = hot(0);
+    if (next_hot) row.load(row.first, next);
+#pragma unroll 1
+    for (int i = 0; i < row.mine; ++i) {
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = next[j];
+      const bool here = next_hot;
+      next_hot = hot(i + 1);
+      if (next_hot) row.load(row.first + i + 1, next);
+      const int i0 = row.first_of(row.first + i), base = i0 - row.lane * kPer;
+      unsigned mask = 0;
+      if (here) {
+        mask = from(w, a.v);
+        if (!plain) {
+#pragma unroll
+          for (int j = 0; j < kPer / 2; ++j) {
+            float lo, hi;
+            two_of<T>(w, j, lo, hi);
+            if (!(lo <= a.most && (lo > a.v || i0 + 2 * j <= a.i))) mask &= ~(1u << (2 * j));
+            if (!(hi <= a.most && (hi > a.v || i0 + 2 * j + 1 <= a.i))) mask &= ~(2u << (2 * j));
+          }
         }
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!any[u]) continue;
-        float x[kPer];
-        widen<T>(w[u], x);
-        f(x, first_of(first + i0 + u));
+      const bool ends = ((i + 1) & ((1 << row.log_q) - 1)) == 0 || i + 1 == row.mine;
+      if (!__any_sync(0xffffffffu, mask != 0)) {
+        if (ends) {
+          if (row.log_q > 0) of_part = warp_sum(of_part);
+          if (row.lane == 0) parts[i >> row.log_q] = of_part;
+          acc += of_part;
+          of_part = 0.0;
+        }
+        continue;
       }
-    }
-  }
-  // Adds to `acc` the amounts, and to `n` the number, of a warp's granules' logits that `want` asks for, 32 side by side where they
-  // are few: each lane by itself would form exponentials for one or two lanes at a time.
-  template <bool kWeights, typename Want>
-  __device__ __forceinline__ void add(const float (&x)[kPer], int i0, Want want, double &acc, int &n) const {
-    unsigned mask = 0;
+      const int own = __popc(mask), up_to = warp_scan(own), all = __shfl_sync(0xffffffffu, up_to, 31);
+      int at = up_to - own;
+      if (a.rest == kNone) {
+        // sums alone: two side by side, as one exponential is a long chain
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) mask |= want(x[j], i0 + j) ? 1u << j : 0u;
-    const int own = __popc(mask);
-    n += own;
-    if constexpr (kWeights) {
-      const int all = __reduce_add_sync(0xffffffffu, own);
-      if (all == 0) return;
-      if (all <= kCompact) {
-        float *to = sh->compact[warp];
-        int at = warp_scan(own) - own;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j)
-          if (mask >> j & 1) to[at++] = x[j];
+        for (int j = 0; j < kPer / 2; ++j) {
+          float lo, hi;
+          two_of<T>(w, j, lo, hi);
+          if (mask >> (2 * j) & 1) value[at++] = lo;
+          if (mask >> (2 * j + 1) & 1) value[at++] = hi;
+        }
         __syncwarp();
-        for (int i = lane; i < all; i += 32) acc += weight(to[i]);
-        __syncwarp();
+        if (!a.weights) {
+          of_part += (double)own;
+        } else {
+#pragma unroll 1
+          for (int e = row.lane; e < all; e += 64) {
+            const double one = row.weight(value[e]), two = row.weight(e + 32 < all ? value[e + 32] : kNegInf);
+            of_part += one + two;
+          }
+        }
+        n += own;
       } else {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j)
-          if (mask >> j & 1) acc += weight(x[j]);
+        for (int j = 0; j < kPer / 2; ++j) {
+          float lo, hi;
+          two_of<T>(w, j, lo, hi);
+          if (mask >> (2 * j) & 1) {
+            value[at] = lo;
+            place[at++] = (uint16_t)(row.lane * kPer + 2 * j);
+          }
+          if (mask >> (2 * j + 1) & 1) {
+            value[at] = hi;
+            place[at++] = (uint16_t)(row.lane * kPer + 2 * j + 1);
+          }
+        }
+        __syncwarp();
+#pragma unroll 1
+        for (int e = row.lane; e < all; e += 32) {
+          const float v = value[e];
+          if (v > a.split) {
+            of_part += a.weights ? row.weight(v) : 1.0;
+            ++n;
+          } else {
+            const int at_row = base + place[e];
+            if (a.rest == kFirst) {
+              best = min(best, at_row);
+            } else if (a.rest == kBinsOfKeys) {
+              atomicAdd(&sh->hist[(a.k_hi - key_of(v)) >> a.shift], 1u);
+            } else if (a.rest == kToList) {
+              row.to_list(v, at_row);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (ends) {
+        of_part = warp_sum(of_part);
+        if (row.lane == 0) parts[i >> row.log_q] = of_part;
+        acc += of_part;
+        of_part = 0.0;
+      }
+    }
+    const bool first = a.rest == kFirst;
+    n = first ? __reduce_min_sync(0xffffffffu, best) : __reduce_add_sync(0xffffffffu, n);
+    __syncthreads();  // chunk and warp_n have been read
+    if (row.lane == 0) {
+      sh->chunk[row.warp] = acc;
+      sh->warp_n[row.warp] = (uint32_t)n;
+    }
+    __syncthreads();
+    const int ns = (int)sh->warp_n[row.lane & (kWarps - 1)];
+    n = first ? __reduce_min_sync(0xffffffffu, ns) : __reduce_add_sync(0xffffffffu, row.lane < kWarps ? ns : 0);
+    Sum r;
+    r.all = warp_sum(row.lane < kWarps ? sh->chunk[row.lane & (kWarps - 1)] : 0.0);
+    r.n = n;
+    if (row.blocks > 1) {
+      row.turn ^= 1;
+      if (threadIdx.x == 0) sh->slot[row.turn] = Slot{r.all, 0.f, n};
+      row.meet();
+      const Slot o = row.told(row.lane & (row.blocks - 1));
+      r.all = warp_sum(row.lane < row.blocks ? o.a : 0.0);
+      r.n = first ? __reduce_min_sync(0xffffffffu, o.i) : __reduce_add_sync(0xffffffffu, row.lane < row.blocks ? o.i : 0);
+    }
+    return r;
+  }
+  __device__ __forceinline__ Sum sum(const Pass &a) {
+    const Sum r = pass(*this, a);
+    if (blocks > 1) turn ^= 1;  // as the pass has told the blocks
+    return r;
+  }
+  // The histogram of the distances of what is kept, none below `low`: most of a row's logits, one by one.
+  __device__ __noinline__ static void bins_of_distance(Row row, float low, float per) {
+    uint32_t *hist = row.sh->hist;
+    const auto hot = [&](int i) {
+      return i < row.mine && (!row.bounds || __uint_as_float((uint32_t)row.bounds[(row.first + i) * 32 + row.lane] << 16) >= low);
+    };
+    const bool plain = low > row.cut_v || row.cut_i == kNoIndex;
+    const float v = fmaxf(low, row.cut_v);
+    uint32_t next[8];
+    bool next_hot = hot(0);
+    if (next_hot) row.load(row.first, next);
+#pragma unroll 1
+    for (int i = 0; i < row.mine; ++i) {
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = next[j];
+      const bool here = next_hot;
+      next_hot = hot(i + 1);
+      if (next_hot) row.load(row.first + i + 1, next);
+      if (!here) continue;
+      const int i0 = row.first_of(row.first + i);
+#pragma unroll
+      for (int j = 0; j < kPer / 2; ++j) {
+        float lo, hi;
+        two_of<T>(w, j, lo, hi);
+        if (lo >= v && (plain || row.kept(lo, i0 + 2 * j))) atomicAdd(&hist[row.bin_of(lo, per)], 1u);
+        if (hi >= v && (plain || row.kept(hi, i0 + 2 * j + 1))) atomicAdd(&hist[row.bin_of(hi, per)], 1u);
       }
     }
   }
-  // Leaves the warp's amounts in `chunk`; the block's number in all threads.
-  template <bool kWeights>
-  __device__ int end_of_sum(double acc, int n) {
-    n = __reduce_add_sync(0xffffffffu, n);
-    const double sum = kWeights ? warp_sum(acc) : (double)n;
-    __syncthreads();  // chunk and warp_n have been read
-    if (lane == 0) {
-      sh->chunk[warp] = sum;
-      sh->warp_n[warp] = (uint32_t)n;
-    }
-    __syncthreads();
-    return __reduce_add_sync(0xffffffffu, lane < kWarps ? (int)sh->warp_n[lane & (kWarps - 1)] : 0);
-  }
-  // The sum of the warps' parts, the block's in a fixed order and the row's, with the row's number; tells the blocks both.
-  __device__ __forceinline__ double sum_of_row(int n, int &all_n) {
+  // The sum of the warps' parts that lie in `chunk`.
+  __device__ __forceinline__ double sum_of_chunks() {
     double v = warp_sum(lane < kWarps ? sh->chunk[lane & (kWarps - 1)] : 0.0);
-    all_n = n;
     if (blocks > 1) {
-      tell(v, 0.f, n);
-      const Slot o = told(lane & (blocks - 1));
-      v = warp_sum(lane < blocks ? o.a : 0.0);
-      all_n = __reduce_add_sync(0xffffffffu, lane < blocks ? o.i : 0);
+      tell(v, 0.f, 0);
+      v = warp_sum(lane < blocks ? told(lane & (blocks - 1)).a : 0.0);
     }
     return v;
   }
-  // The sum of the weights that `want` asks for, in double.
-  template <typename Want>
-  __device__ double sum_of(float floor, Want want, int &all_n) {
-    double acc = 0.0;
-    int n = 0;
-    sweep(floor, [&](const float (&x)[kPer], int i0) { add<true>(x, i0, want, acc, n); });
-    n = end_of_sum<true>(acc, n);
-    return sum_of_row(n, all_n);
-  }
-  // The whole row's.
-  __device__ double whole() {
-    int n;
-    return sum_of(kLowest, [](float x, int) { return x > kNegInf; }, n);
-  }
+  // The whole row's, in double.
+  __device__ __forceinline__ double whole() { return sum(Pass{kLowest, kNoIndex, -kNegInf, kNegInf, true, kNone, 0, 0}).all; }
 
-  // The first index of the maximum.
-  __device__ int first_of_max() {
-    int best = kNoIndex;
-    sweep(m, [&](const float (&x)[kPer], int i0) {
-#pragma unroll
-      for (int j = kPer - 1; j >= 0; --j)
-        if (x[j] == m) best = min(best, i0 + j);
-    });
-    best = __reduce_min_sync(0xffffffffu, best);
-    __syncthreads();
-    if (lane == 0) sh->warp_n[warp] = (uint32_t)best;
-    __syncthreads();
-    best = __reduce_min_sync(0xffffffffu, lane < kWarps ? (int)sh->warp_n[lane & (kWarps - 1)] : kNoIndex);
-    if (blocks > 1) {
-      tell(0.0, 0.f, best);
-      best = __reduce_min_sync(0xffffffffu, told(lane & (blocks - 1)).i);
-    }
-    return best;
-  }
-
-  // The index at which the running sum over the row passes `aim`, where the warps' parts lie in `chunk` and the blocks' have been told
-  // (sum_of_row): the first in `want` where it does, or the last of those with something where rounding leaves none.  Known to
-  // the block that has it alone; the others get -2.  `unsure`: how far the running sums may be off; then the answer is
+  // The index at which the running sum of a pass `a` over the row passes `aim`, where the warps' parts lie in `chunk` and the blocks'
+  // have been told: the first that it looks for where it does, or the last of those with something where rounding leaves none.
+  // Known to the block that has it alone; the others get -2.  `unsure`: how far the parts may be off; then the answer is
   // kNoIndex where that matters, known to all.
-  template <bool kWeights, typename Want>
-  __device__ int find(double aim, Want want, double unsure = 0.0) {
-    const auto amount = [&](float x) { return kWeights ? weight(x) : 1.0; };
+  __device__ __noinline__ static int find(Row row, const Pass a, double aim, double unsure, bool pairs) {
+    Shared *sh = row.sh;
+    const int lane = row.lane, blocks = row.blocks;
+    const auto amount = [&](float x, int i) {
+      if (!(x >= a.v && x <= a.most && (x > a.v || i <= a.i))) return 0.0;
+      return a.weights ? row.weight(x) : 1.0;
+    };
+    // where the running sum, `run` in front of lane 0, passes: the lane, or the last with something (-1); moves `run` in front of it
+    bool hit = true;
+    const auto passes = [&](double part, double &run) {
+      const double up_to = warp_scan(part);
+      const unsigned over = __ballot_sync(0xffffffffu, run + up_to > aim && part > 0.0), some = __ballot_sync(0xffffffffu, part > 0.0);
+      const int who = over ? __ffs(over) - 1 : 31 - __clz(some);
+      hit = over != 0;
+      if (who >= 0) run += __shfl_sync(0xffffffffu, up_to - part, who);
+      return who;
+    };
+    double run = 0.0;
     int owner = 0;
-    double before = 0.0;
-    if (blocks > 1) {
-      const double part = lane < blocks ? told(lane & (blocks - 1)).a : 0.0, up_to = warp_scan(part);
-      const unsigned passes = __ballot_sync(0xffffffffu, lane < blocks && up_to > aim && part > 0.0);
-      const unsigned any = __ballot_sync(0xffffffffu, part > 0.0);
-      owner = passes ? __ffs(passes) - 1 : 31 - __clz(any);
-      before = __shfl_sync(0xffffffffu, up_to - part, owner);
-    }
+    if (blocks > 1) owner = max(0, passes(lane < blocks ? row.told(lane & (blocks - 1)).a : 0.0, run));
     int at = -2;
-    if (owner == rank) {
+    if (owner == row.rank) {
       // the warp whose part it is
-      const double part = lane < kWarps ? sh->chunk[lane & (kWarps - 1)] : 0.0, up_to = warp_scan(part);
-      const unsigned passes = __ballot_sync(0xffffffffu, lane < kWarps && before + up_to > aim && part > 0.0);
-      const unsigned any = __ballot_sync(0xffffffffu, part > 0.0);
-      const int of_warp = passes ? __ffs(passes) - 1 : 31 - __clz(any);
-      double run = before + __shfl_sync(0xffffffffu, up_to - part, of_warp);
-      const int per = (segs + kWarps - 1) / kWarps, s0 = of_warp * per, s1 = min(segs, s0 + per);
-      // its pieces' sums, by all warps, kSegs at a time
-      int piece = -1, last = -1;
-      double run_last = run;
-      for (int p0 = s0; p0 < s1 && piece < 0; p0 += kSegs) {
-        const int p1 = min(s1, p0 + kSegs);
-        __syncthreads();
-        for (int seg = p0 + warp; seg < p1; seg += kWarps) {
-          uint32_t w[8];
-          load(seg, w);
-          float x[kPer];
-          widen<T>(w, x);
-          const int i0 = first_of(seg);
-          double g = 0.0;
-#pragma unroll
-          for (int j = 0; j < kPer; ++j)
-            if (want(x[j], i0 + j)) g += amount(x[j]);
-          g = warp_sum(g);
-          if (lane == 0) sh->seg[seg - p0] = g;
-        }
-        __syncthreads();
-        // every warp alike
-        for (int q = p0; q < p1 && piece < 0; q += 32) {
-          const double part = q + lane < p1 ? sh->seg[q + lane - p0] : 0.0, up = warp_scan(part);
-          const unsigned hit = __ballot_sync(0xffffffffu, run + up > aim && part > 0.0), some = __ballot_sync(0xffffffffu, part > 0.0);
-          const int who = hit ? __ffs(hit) - 1 : some ? 31 - __clz(some) : -1;
-          if (who >= 0) {
-            last = q + who;
-            run_last = run + __shfl_sync(0xffffffffu, up - part, who);
-            if (hit) piece = last;
+      const int of_warp = max(0, passes(lane < kWarps ? sh->chunk[lane & (kWarps - 1)] : 0.0, run));
+      const int per = (row.segs + kWarps - 1) / kWarps, s0 = of_warp * per, s1 = min(row.segs, s0 + per);
+      // its parts, every warp alike
+      int part_of = 0, piece = -1;
+      {
+        const int parts = (s1 - s0 + (1 << row.log_q) - 1) >> row.log_q;
+        const double *stored = sh->part[of_warp];
+        double run_last = run;
+#pragma unroll 1
+        for (int q = 0; q < parts && piece < 0; q += 32) {
+          double part = q + lane < parts ? stored[q + lane] : 0.0;
+          if (pairs && q + lane < parts) {
+            const float top = __int_as_float(__double2hiint(part));
+            part = top > kNegInf ? (double)__int_as_float(__double2loint(part)) * row.power(((double)top - (double)row.m) * row.inv_t) : 0.0;
           }
-          run += __shfl_sync(0xffffffffu, up, 31);
+          const double end = run + warp_sum(part);
+          const int who = passes(part, run);
+          if (who >= 0) {
+            part_of = q + who;
+            run_last = run;
+            if (hit) piece = part_of;
+          }
+          run = end;
         }
+        run = run_last;
+      }
+      int last = s0 + (part_of << row.log_q);
+      if (row.log_q > 0) {
+        // the part's pieces one by one
+        const int end = min(s1, last + (1 << row.log_q));
+        double run_last = run;
+        bool found_piece = false;
+#pragma unroll 1
+        for (int seg = last; seg < end && !found_piece; ++seg) {
+          double g = 0.0;
+#pragma unroll 1
+          for (int j = 0; j < kPer; ++j) {
+            const int i = row.first_of(seg) - lane * kPer + lane + 32 * j;
+            if (i >= 0 && i < row.V) g += amount(Storage<T>::widen(row.z[i]), i);
+          }
+          g = warp_sum(g);
+          if (g > 0.0) {
+            last = seg;
+            run_last = run;
+            found_piece = run + g > aim;
+          }
+          run += g;
+        }
+        run = run_last;
+        if (!found_piece) piece = -1;
       }
       bool clear = piece >= 0;
-      // the granule, then the logit: a lane each
-      run = run_last;
-      last = max(last, s0);
-      uint32_t w[8];
-      load(last, w);
-      float x[kPer];
-      widen<T>(w, x);
-      int i0 = first_of(last);
-      double g = 0.0;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (want(x[j], i0 + j)) g += amount(x[j]);
-      double up = warp_scan(g);
-      unsigned hit = __ballot_sync(0xffffffffu, run + up > aim && g > 0.0);
-      unsigned some = __ballot_sync(0xffffffffu, g > 0.0);
-      int who = max(0, hit ? __ffs(hit) - 1 : 31 - __clz(some));
+      // its 32s of logits, a warp each, then the logit
+      const int i0 = row.first_of(last) - lane * kPer;
+      const auto term = [&](int group) {
+        const int i = i0 + group * 32 + lane;
+        return i >= 0 && i < row.V ? amount(Storage<T>::widen(row.z[i]), i) : 0.0;
+      };
+#pragma unroll 1
+      for (int g = row.warp; g < kPer; g += kWarps) {
+        const double all = warp_sum(term(g));
+        if (lane == 0) sh->group[g] = all;
+      }
+      __syncthreads();
+      const int group = max(0, passes(lane < kPer ? sh->group[lane] : 0.0, run));
       clear = clear && hit;
-      run += __shfl_sync(0xffffffffu, up - g, who);
-      i0 = __shfl_sync(0xffffffffu, i0, who);
-      const int i = i0 + lane;
-      const float v = lane < kPer && i >= 0 && i < V ? Storage<T>::widen(z[i]) : kNegInf;
-      g = v > kNegInf && want(v, i) ? amount(v) : 0.0;
-      up = warp_scan(g);
-      hit = __ballot_sync(0xffffffffu, run + up > aim && g > 0.0);
-      some = __ballot_sync(0xffffffffu, g > 0.0);
-      who = max(0, hit ? __ffs(hit) - 1 : 31 - __clz(some));
-      const double low = run + __shfl_sync(0xffffffffu, up - g, who), high = run + __shfl_sync(0xffffffffu, up, who);
-      at = min(max(i0 + who, 0), V - 1);
-      if (unsure > 0.0 && !(clear && hit && low + unsure <= aim && high - unsure > aim)) at = kNoIndex;
-    }
-    if (unsure > 0.0 && blocks > 1) {
-      tell(0.0, 0.f, at);
-      if (told(owner).i == kNoIndex) return kNoIndex;
+      const double g = term(group);
+      const int who = max(0, passes(g, run));
+      const double v = __shfl_sync(0xffffffffu, g, who);
+      at = min(max(i0 + group * 32 + who, 0), row.V - 1);
+      if (unsure > 0.0 && !(clear && hit && run + unsure <= aim && run + v - unsure > aim)) at = kNoIndex;
     }
     return at;
   }
-  // find(), known to all blocks.
-  template <bool kWeights, typename Want>
-  __device__ int find_for_all(double aim, Want want) {
-    int at = find<kWeights>(aim, want);
-    if (blocks > 1) {
+  // find(), and whether it failed, known to all blocks; `everywhere`: the index too.
+  __device__ __forceinline__ int found(const Pass &a, double aim, double unsure, bool everywhere, bool pairs) {
+    int at = find(*this, a, aim, unsure, pairs);
+    if ((everywhere || unsure > 0.0) && blocks > 1) {
       tell(0.0, 0.f, at);
-      at = __reduce_max_sync(0xffffffffu, told(lane & (blocks - 1)).i);
+      const int any = __reduce_max_sync(0xffffffffu, told(lane & (blocks - 1)).i);
+      if (everywhere || any == kNoIndex) at = any;
     }
     return at;
   }
@@ -537,7 +762,7 @@ struct Row {
   // ---- 2: the cut
   // Logits in the order of the row lie in bins by their distance from the maximum; the last bin has all from kBins - 1 on.
   __device__ __forceinline__ int bin_of(float x, float per) const {
-    return min(kBins - 1, __float2int_rz(fminf(fminf(m - x, -kLowest) * per, 1e9f)));
+    return min(kBins - 1, __float2int_rz((m - x) * per));  // the conversion saturates; infinity times 0 is bin 0 as all the others
   }
 
   // A lower bound of the k-th largest logit from the granules' maxima: where k granules reach up to a value, k logits do.
@@ -580,12 +805,10 @@ struct Row {
     return low;
   }
 
-  // Moves the cut to the last logit, in falling order, before which less than share * all lies; kWeights: sums of weights, else
+  // Moves the cut to the last logit, in falling order, before which less than share * all lies; weights: sums of weights, else
   // of ones.  Logits below `floor` are known to lie behind it.  `all`: the amount in the whole row, good to `unsure`, of which at
-  // most `below` lies below `floor`.  Returns whether the weights of what is kept lie in `chunk` and their number in `n`.
-  template <bool kWeights>
-  __device__ bool select(double share, double all, double unsure, float floor, double below, int &n_kept) {
-    const auto amount = [&](float x) { return kWeights ? weight(x) : 1.0; };
+  // most `below` lies below `floor`.
+  __device__ void select(bool weights, double share, double all, double unsure, float floor, double below) {
     double aim = share * all;
     const float span = floor > 0.5f * kLowest ? m - floor : (float)(40.0 / inv_t);
     const float most = (float)(kBins - 2) / span, per = span > 0.f && most < 1e30f ? most : 0.f;  // 0: all in one bin
@@ -593,6 +816,7 @@ struct Row {
     float low = floor, high = m;
     uint32_t n_in = 0;
     // every level divides the keys by 2,048, at the latest from the eighth on: eleven are the most
+#pragma unroll 1
     for (int level = 0; level < 16; ++level) {
       const uint32_t k_lo = key_of(low), k_hi = key_of(high), width = k_hi - k_lo;
       const int shift = max(0, 21 - __clz(width));  // (width >> shift) < kBins
@@ -605,122 +829,91 @@ struct Row {
         unsure = 0.0;
       }
       __syncthreads();
-      if (!gather)
-        for (int i = threadIdx.x; i < kBins; i += kThreads) sh->hist[i] = 0;
+      for (int i = threadIdx.x; i < kBins; i += kThreads) sh->hist[i] = 0;
       if (threadIdx.x == 0) sh->list_n = 0;
       __syncthreads();
-      double above = 0.0;
-      int n_above = 0, n_block = 0;
+      Pass a = of_kept(low);
+      a.weights = weights;
+      a.split = high;  // only the logits above; what is cut already lies at the bracket's end or behind it
+      a.rest = ties ? kNone : gather ? kToList : kBinsOfKeys;
+      if (ties) a.v = high, a.i = -1;
+      a.k_hi = k_hi;
+      a.shift = shift;
+      Sum above = {0.0, 0};
+      double tail = 0.0;
       if (level == 0) {
-        sweep(low, [&](const float (&x)[kPer], int i0) {
-#pragma unroll
-          for (int j = 0; j < kPer; ++j)
-            if (x[j] >= low && kept(x[j], i0 + j)) atomicAdd(&sh->hist[bin_of(x[j], per)], 1u);
-        });
+        bins_of_distance(*this, low, per);
         meet();
+      } else if (gather && unsure > 0.0) {
+        tail = behind(low, high);
       } else {
-        // the amount in front of the bracket, and the bracket's logits in bins or in the list
-        double acc = 0.0;
-        sweep(low, [&](const float (&x)[kPer], int i0) {
-          // what is cut already lies at the bracket's end or behind it
-          add<kWeights>(x, i0, [&](float v, int) { return v > high; }, acc, n_block);
-          if (ties) return;
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) {
-            if (!(x[j] >= low && x[j] <= high && kept(x[j], i0 + j))) continue;
-            if (gather) {
-              const uint32_t at = atomicAdd(&sh->list_n, 1u);
-              if (at < kList) sh->list[at] = (uint64_t)(~key_of(x[j])) << 32 | (uint32_t)(i0 + j);
-            } else {
-              atomicAdd(&sh->hist[(k_hi - key_of(x[j])) >> shift], 1u);
-            }
-          }
-        });
-        n_block = end_of_sum<kWeights>(acc, n_block);
-        above = sum_of_row(n_block, n_above);
+        above = sum(a);
       }
       if (ties) {
         // kept are the first r with above + (r - 1) w < aim
-        const double w = amount(high);
+        const double w = weights ? weight(high) : 1.0;
         const auto number = [&](double to) {
-          double r = fmin((double)n_in, fmax(1.0, ceil((to - above) / w)));
-          if (r > 1.0 && !(above + (r - 1.0) * w < to))
+          double r = fmin((double)n_in, fmax(1.0, ceil((to - above.all) / w)));
+          if (r > 1.0 && !(above.all + (r - 1.0) * w < to))
             r -= 1.0;
-          else if (r < (double)n_in && above + r * w < to)
+          else if (r < (double)n_in && above.all + r * w < to)
             r += 1.0;
           return r;
         };
-        double r = number(aim);
-        if (unsure > 0.0 && number(share * (all - unsure)) != number(share * (all + unsure))) r = number(share * whole());
-        const auto tie = [&](float x, int i) { return x == high && kept(x, i); };
-        double acc = 0.0;
-        int n = 0, row_n;
-        sweep(high, [&](const float (&x)[kPer], int i0) { add<false>(x, i0, tie, acc, n); });
-        n = end_of_sum<false>(acc, n);
-        sum_of_row(n, row_n);
-        const int at = find_for_all<false>(r - 0.5, tie);
+        const double r = number(aim);
+        a = of_kept(high);
+        a.most = high;
+        a.weights = false;
+        sum(a);
+        cut_i = found(a, r - 0.5, 0.0, true, false);
         cut_v = high;
-        cut_i = at;
-        return false;
+        return;
       }
       if (gather) {
         // all blocks' lists in one, alike in every block
         int n = 0;
-        if (blocks == 1) {
-          n = (int)sh->list_n;
-          if (n <= kList)
-            for (int i = threadIdx.x; i < n; i += kThreads) sh->sorted[i] = sh->list[i];
-        } else {
-          for (int r = 0; r < blocks; ++r) {
-            const Shared *o = of(r);
-            const int k = (int)o->list_n;
-            if (n + k <= kList)
-              for (int i = threadIdx.x; i < k; i += kThreads) sh->sorted[n + i] = o->list[i];
-            n += k;
-          }
-          meet();  // the lists have been read
+#pragma unroll 1
+        for (int r = 0; r < blocks; ++r) {
+          const Shared *o = r == rank ? sh : of(r);
+          const int k = (int)o->list_n;
+          if (n + k <= kList)
+            for (int i = threadIdx.x; i < k; i += kThreads) sh->sorted[n + i] = o->list[i];
+          n += k;
         }
-        if (n > kList) {  // more on the bracket's edge than its bins had
+        if (blocks > 1) meet();  // the lists have been read
+        if (n > kList) {         // more on the bracket's edge than its bins had
           n_in = (uint32_t)n;
           continue;
         }
         sort_list(n);
         int last;
-        double list_sum;
-        if (!cut_from_list<kWeights>(n, aim, share * unsure, above, last, list_sum)) {
-          // the float32 sum is not enough: what lies behind the bracket in float32 again, beside the rest in double, mostly is
-          const double tail = behind(low);
-          if (!cut_from_list<kWeights>(n, share * (above + list_sum + tail), 4.0 * share * tail * eps() /* exponents of up to 126 */,
-                                       above, last, list_sum)) {
-            // the sum of what is above is in `chunk` no more
-            const double exact = whole();
-            cut_from_list<kWeights>(n, share * exact, 0.0, above, last, list_sum);
-            set_cut(last);
-            return false;
+        if (unsure > 0.0) {
+          // Kept is what has more than (1 - share) all at and behind it.  Of that side's sums, the whole's and the tail's, float32's
+          // errors are the smaller by 1 - share; mostly nothing lies so near the border that they matter.
+          const double end = (1.0 - share) * all;
+          if (!cut_from_list(true, n, tail - end, true, (1.0 - share) * unsure + tail * eps(tail), last)) {
+            for (int i = threadIdx.x; i < n; i += kThreads) sh->list[i] = sh->sorted[i];  // passes take their place
+            __syncthreads();
+            aim = share * whole();
+            a.v = high;
+            a.i = -1;
+            a.rest = kNone;
+            above = sum(a);
+            for (int i = threadIdx.x; i < n; i += kThreads) sh->sorted[i] = sh->list[i];
+            __syncthreads();
+            cut_from_list(true, n, aim - above.all, false, 0.0, last);
           }
+        } else {
+          cut_from_list(weights, n, aim - above.all, false, 0.0, last);
         }
         set_cut(last);
-        if (!kWeights) return false;
-        // the list's kept logits to the warps that have their pieces
-        const int each = (segs + kWarps - 1) / kWarps;
-        const int lo_i = (seg0 + warp * each) * 32 * kPer - off, hi_i = (seg0 + min(segs, (warp + 1) * each)) * 32 * kPer - off;
-        double acc = 0.0;
-        for (int i = lane; i <= last; i += 32) {
-          const uint64_t item = sh->sorted[i];
-          const int at = (int)(uint32_t)item;
-          if (at >= lo_i && at < hi_i) acc += weight(value_of(~(uint32_t)(item >> 32)));
-        }
-        acc = warp_sum(acc);
-        if (lane == 0) sh->chunk[warp] += acc;
-        n_kept = n_above + last + 1;
-        __syncthreads();
-        return true;
+        return;
       }
-      bracket<kWeights>(level, aim, above, all, share * unsure, below, unsure, per, k_lo, k_hi, shift);
+      bracket(weights, level, aim, above.all, all, share * unsure, below, unsure, per, k_lo, k_hi, shift);
       const uint32_t lo = sh->pick_lo, hi = sh->pick_hi;
       n_in = sh->pick_last;
       meet();  // the histograms have been read
-      if (n_in == 0) return false;  // less than the aim in all: everything stays
+      if (n_in == 0) return;  // less than the aim in all: everything stays
       if (level == 0) {
         // the values that the bins' logits can have; 2^-20 covers the roundings of the distance
         const double slack = 9.5367431640625e-7;
@@ -733,24 +926,52 @@ struct Row {
         high = value_of(k_hi - (lo << shift));
       }
     }
-    return false;
   }
   __device__ __forceinline__ void set_cut(int last) {
     const uint64_t item = sh->sorted[last];
     cut_v = value_of(~(uint32_t)(item >> 32));
     cut_i = (int)(uint32_t)item;
   }
-  // The float32 sum of the weights of logits below `low`, of a row that nothing is cut from.  Leaves `chunk` alone.
-  __device__ double behind(float low) {
-    float s = 0.f;
-    sweep(kLowest, [&](const float (&x)[kPer], int) {
-      float g = 0.f;
+  __device__ __forceinline__ void to_list(float x, int i) const {
+    const uint32_t to = atomicAdd(&sh->list_n, 1u);
+    if (to < kList) sh->list[to] = (uint64_t)(~key_of(x)) << 32 | (uint32_t)i;
+  }
+  // Of a row that nothing is cut from: the float32 sum of the weights of logits below `low`, with what lies from there to `high` to
+  // the list.  Leaves `chunk` alone.
+  __device__ __noinline__ static double behind_of_warp(const Row row, float low, float high) { return row.sweep_behind(low, high); }
+  __device__ __forceinline__ double sweep_behind(float low, float high) const {
+    double s = 0.0;
+    uint32_t next[8];
+    if (mine > 0) load(first, next);
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+      uint32_t w[8];
 #pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (x[j] < low) g += ex2((x[j] - m) * c);
-      s += g;
-    });
-    const double ws = warp_sum((double)s);
+      for (int j = 0; j < 8; ++j) w[j] = next[j];
+      if (i + 1 < mine) load(first + i + 1, next);
+      const int i0 = first_of(first + i);
+      unsigned out = 0, in = 0;  // not in the sum; in the list
+#pragma unroll
+      for (int j = 0; j < kPer / 2; ++j) {
+        float a, b;
+        two_of<T>(w, j, a, b);
+        out |= (a < low && !((a - m) * c < -1e4f) ? 0u : 1u) << (2 * j) | (b < low && !((b - m) * c < -1e4f) ? 0u : 1u) << (2 * j + 1);
+        in |= (a >= low && a <= high ? 1u : 0u) << (2 * j) | (b >= low && b <= high ? 1u : 0u) << (2 * j + 1);
+      }
+      s += (double)terms<true>(w, m, out);
+      if (!__any_sync(0xffffffffu, in != 0)) continue;
+#pragma unroll
+      for (int j = 0; j < kPer / 2; ++j) {
+        float a, b;
+        two_of<T>(w, j, a, b);
+        if (in >> (2 * j) & 1) to_list(a, i0 + 2 * j);
+        if (in >> (2 * j + 1) & 1) to_list(b, i0 + 2 * j + 1);
+      }
+    }
+    return warp_sum(s);
+  }
+  __device__ double behind(float low, float high) {
+    const double ws = behind_of_warp(*this, low, high);
     __syncthreads();
     if (lane == 0) sh->warp_a[warp] = ws;
     __syncthreads();
@@ -761,7 +982,6 @@ struct Row {
     }
     return own;
   }
-
   // The least key of bin b, of keys from k_lo to k_hi: bin 0 has the largest.
   __device__ __forceinline__ static uint32_t edge_of(uint32_t k_lo, uint32_t k_hi, uint32_t b, int shift) {
     const int64_t least = (int64_t)k_hi - (int64_t)(((uint64_t)b + 1) << shift) + 1;
@@ -770,47 +990,48 @@ struct Row {
 
   // Which of the histograms' bins can hold the cut, whose aim is good to `unsure`: pick_lo to pick_hi, which have pick_last logits (0:
   // all of it lies in front of the aim).  Every block alike.
-  template <bool kWeights>
-  __device__ void bracket(int level, double aim, double above, double all, double unsure, double below, double all_unsure, float per,
+  __device__ void bracket(bool weights, int level, double aim, double above, double all, double unsure, double below, double all_unsure, float per,
                           uint32_t k_lo, uint32_t k_hi, int shift) {
     constexpr int kOwn = kBins / kThreads;
     // where a bin holds one value, or the bracket would not get smaller, the larger bound decides
-    const bool sharp = !kWeights || level >= 8 || (level > 1 && shift == 0);
-    uint32_t n[kOwn], n_sum = 0;
+    const bool sharp = !weights || level >= 8 || (level > 1 && shift == 0);
+    uint32_t n[kOwn];
     double least[kOwn], most[kOwn], least_sum = 0.0, most_sum = 0.0;
+    static_assert(kOwn % 4 == 0, "bins are read four at a time");
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) n[j] = sh->hist[threadIdx.x * kOwn + j];
-    for (int r = 1; r < blocks; ++r) {
-      const Shared *o = of((rank + r) & (blocks - 1));
+    for (int j = 0; j < kOwn; ++j) n[j] = 0;
+#pragma unroll 1
+    for (int r = 0; r < blocks; ++r) {
+      const uint32_t *hist = (r ? of((rank + r) & (blocks - 1)) : sh)->hist + threadIdx.x * kOwn;
 #pragma unroll
-      for (int j = 0; j < kOwn; ++j) n[j] += o->hist[threadIdx.x * kOwn + j];
+      for (int j = 0; j < kOwn; j += 4) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(hist + j);
+        n[j] += q.x, n[j + 1] += q.y, n[j + 2] += q.z, n[j + 3] += q.w;
+      }
     }
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const uint32_t b = threadIdx.x * kOwn + j;
       least[j] = most[j] = (double)n[j];
-      if (kWeights && n[j]) {
-        double far, near;  // the bin's distances from the maximum
+      if (weights && n[j]) {
         if (level == 0) {
-          const double slack = 9.5367431640625e-7;
-          near = per > 0.f ? (double)b / per * (1.0 - slack) : 0.0;
-          far = b == kBins - 1 || per == 0.f ? __longlong_as_double(0x7ff0000000000000LL) : ((double)b + 1.0) / per * (1.0 + slack);
+          // the bin's distances from the maximum; 2^-20 and 1e-5 cover the roundings
+          const float near = (float)b / per * (1.f - 1e-6f), far = ((float)b + 1.f) / per * (1.f + 1e-6f);
+          most[j] *= per > 0.f ? (double)ex2(-near * c) * (1.0 + 1e-5) : 1.0;
+          least[j] *= b == kBins - 1 || per == 0.f ? 0.0 : (double)ex2(-far * c) * (1.0 - 1e-5);
         } else {
-          near = (double)m - (double)value_of(k_hi - (b << shift));
-          far = (double)m - (double)value_of(edge_of(k_lo, k_hi, b, shift));
+          const double near = (double)m - (double)value_of(k_hi - (b << shift));
+          const double far = (double)m - (double)value_of(edge_of(k_lo, k_hi, b, shift));
+          most[j] *= power(-near * inv_t);
+          least[j] = sharp ? most[j] : least[j] * power(-far * inv_t);
         }
-        most[j] *= exp(-near * inv_t);
-        least[j] = sharp ? most[j] : least[j] * exp(-far * inv_t);
       }
-      n_sum += n[j];
       least_sum += least[j];
       most_sum += most[j];
     }
-    const uint32_t n_up = warp_scan(n_sum);
     const double least_up = warp_scan(least_sum), most_up = warp_scan(most_sum);
     __syncthreads();
     if (lane == 31) {
-      sh->warp_n[warp] = n_up;
       sh->warp_a[warp] = least_up;
       sh->warp_b[warp] = most_up;
     }
@@ -820,16 +1041,14 @@ struct Row {
       sh->pick_last = 0;     // the last that holds anything
     }
     __syncthreads();
-    double least_run = above + least_up - least_sum, most_run = above + most_up - most_sum, least_all = above, most_all = above + below;
-    for (int w = 0; w < kWarps; ++w) {
-      const double a = sh->warp_a[w], b = sh->warp_b[w];
-      if (w < warp) {
-        least_run += a;
-        most_run += b;
-      }
-      least_all += a;
-      most_all += b;
-    }
+    // the warps in front of this one, and all
+    const double la = warp_scan(lane < kWarps ? sh->warp_a[lane & (kWarps - 1)] : 0.0);
+    const double lb = warp_scan(lane < kWarps ? sh->warp_b[lane & (kWarps - 1)] : 0.0);
+    const double a_before = __shfl_sync(0xffffffffu, la, max(warp - 1, 0)), b_before = __shfl_sync(0xffffffffu, lb, max(warp - 1, 0));
+    double least_run = above + (warp ? a_before : 0.0) + (least_up - least_sum);
+    double most_run = above + (warp ? b_before : 0.0) + (most_up - most_sum);
+    const double least_all = above + __shfl_sync(0xffffffffu, la, 31), most_all = above + below + __shfl_sync(0xffffffffu, lb, 31);
+    uint32_t first_lo = kBins, first_hi = kBins, last_any = 0;
     // A bin's edges bound its weights to a percent or so.  Over the whole row (level 0) the bounds on what lies behind a bin,
     // taken from the known whole, are the closer ones where the aim is near it: 1.5 % of the last twentieth for a top_p of 0.95
     const double eps = sharp ? 0.0 : 1e-11 * all + unsure;
@@ -839,14 +1058,22 @@ struct Row {
       least_run += least[j];
       most_run += most[j];
       if (!n[j]) continue;
-      atomicMax(&sh->pick_last, b);
+      last_any = b;
       double high = most_run, low = sharp ? most_run : least_run;
       if (!sharp && level == 0) {
         high = fmin(high, all + all_unsure - (least_all - least_run));
         low = fmax(low, all - all_unsure - (most_all - most_run));
       }
-      if (high >= aim - eps) atomicMin(&sh->pick_lo, b);
-      if (low >= aim + eps) atomicMin(&sh->pick_hi, b);
+      if (high >= aim - eps) first_lo = min(first_lo, b);
+      if (low >= aim + eps) first_hi = min(first_hi, b);
+    }
+    first_lo = __reduce_min_sync(0xffffffffu, first_lo);
+    first_hi = __reduce_min_sync(0xffffffffu, first_hi);
+    last_any = __reduce_max_sync(0xffffffffu, last_any);
+    if (lane == 0) {
+      if (first_lo < (uint32_t)kBins) atomicMin(&sh->pick_lo, first_lo);
+      if (first_hi < (uint32_t)kBins) atomicMin(&sh->pick_hi, first_hi);
+      if (last_any) atomicMax(&sh->pick_last, last_any);
     }
     __syncthreads();
     uint32_t lo = sh->pick_lo, hi = min(sh->pick_hi, (uint32_t)kBins - 1);
@@ -872,12 +1099,44 @@ struct Row {
 
   // Sorts the n items of `sorted`: falling logits, rising indices.
   __device__ void sort_list(int n) {
+    __syncthreads();
+    if (n <= kThreads) {
+      // an item a thread; partners in the same warp are met by shuffles
+      const int i = threadIdx.x;
+      uint64_t x = i < n ? sh->sorted[i] : ~0ull;
+      int size = 32;
+      while (size < n) size <<= 1;
+      const bool in = (i & ~31) < size;
+#pragma unroll 1
+      for (int k = 2; k <= size; k <<= 1)
+#pragma unroll 1
+        for (int j = k >> 1; j > 0; j >>= 1) {
+          uint64_t y;
+          if (j >= 32) {
+            __syncthreads();
+            if (in) sh->sorted[i] = x;
+            __syncthreads();
+            y = in ? sh->sorted[i ^ j] : x;
+          } else {
+            y = __shfl_xor_sync(0xffffffffu, x, j);
+          }
+          const bool low = (i & j) == 0, rising = (i & k) == 0;
+          if ((low == rising) ? y < x : y > x) x = y;
+        }
+      __syncthreads();
+      if (in) sh->sorted[i] = x;
+      __syncthreads();
+      return;
+    }
     int size = 32;
     while (size < n) size <<= 1;
     for (int i = n + threadIdx.x; i < size; i += kThreads) sh->sorted[i] = ~0ull;
     __syncthreads();
+#pragma unroll 1
     for (int k = 2; k <= size; k <<= 1)
+#pragma unroll 1
       for (int j = k >> 1; j > 0; j >>= 1) {
+#pragma unroll 1
         for (int t = threadIdx.x; t < size / 2; t += kThreads) {
           const int a = (t & ~(j - 1)) * 2 + (t & (j - 1)), b = a + j;
           const uint64_t x = sh->sorted[a], y = sh->sorted[b];
@@ -890,52 +1149,48 @@ struct Row {
       }
   }
   // The last of the sorted list before which less than the aim lies; returns whether that is so for every aim within `unsure`.
-  template <bool kWeights>
-  __device__ bool cut_from_list(int n, double aim, double unsure, double above, int &last, double &list_sum) {
+  // `from_end`: the aim is against the list's sum.
+  __device__ bool cut_from_list(bool weights, int n, double aim, bool from_end, double unsure, int &last) {
     constexpr int kOwn = kList / kThreads;
     double w[kOwn], sum = 0.0;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const int i = threadIdx.x * kOwn + j;
-      w[j] = i < n ? kWeights ? weight(value_of(~(uint32_t)(sh->sorted[i] >> 32))) : 1.0 : 0.0;
+      w[j] = i < n ? weights ? weight(value_of(~(uint32_t)(sh->sorted[i] >> 32))) : 1.0 : 0.0;
       sum += w[j];
     }
     const double up_to = warp_scan(sum);
     __syncthreads();
     if (lane == 31) sh->warp_a[warp] = up_to;
-    if (threadIdx.x == 0) {
-      sh->pick_last = 0;
-      sh->unclear = 0;
-    }
     __syncthreads();
-    double run = above + up_to - sum, all = 0.0;
-    for (int v = 0; v < kWarps; ++v) {
-      const double a = sh->warp_a[v];
-      if (v < warp) run += a;
-      all += a;
-    }
+    const double la = warp_scan(lane < kWarps ? sh->warp_a[lane & (kWarps - 1)] : 0.0), before = __shfl_sync(0xffffffffu, la, max(warp - 1, 0));
+    double run = (warp ? before : 0.0) + (up_to - sum);
+    if (from_end) aim += __shfl_sync(0xffffffffu, la, 31);
+    int in_front = 0, unclear = 0;  // of the list, before which less than the aim lies: its front
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const int i = threadIdx.x * kOwn + j;
-      if (i < n && (run < aim || i == 0)) atomicMax(&sh->pick_last, (uint32_t)i);
+      in_front += i < n && (run < aim || i == 0);
       // the bracket holds the cut: its first logit is kept, and its end is behind the aim
-      if (unsure > 0.0 && i < n && i > 0 && fabs(run - aim) <= unsure) sh->unclear = 1;
+      unclear |= unsure > 0.0 && i < n && i > 0 && fabs(run - aim) <= unsure;
       run += w[j];
-      if (unsure > 0.0 && i == n - 1 && run - aim <= unsure) sh->unclear = 1;
+      unclear |= unsure > 0.0 && i == n - 1 && run - aim <= unsure;
     }
-    __syncthreads();
-    last = (int)sh->pick_last;
-    list_sum = all;
-    return sh->unclear == 0;
+    in_front = __reduce_add_sync(0xffffffffu, in_front);
+    if (lane == 0) sh->warp_n[warp] = (uint32_t)in_front;
+    unclear = __syncthreads_or(unclear);
+    last = (int)__reduce_add_sync(0xffffffffu, lane < kWarps ? sh->warp_n[lane & (kWarps - 1)] : 0u) - 1;
+    __syncthreads();  // warp_n and warp_a have been read
+    return !unclear;
   }
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
+__global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Params p) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Row<T> row;
-  row.sh = reinterpret_cast<Shared *>(smem_raw);
-  row.bounds = p.bounds ? reinterpret_cast<uint16_t *>(smem_raw + sizeof(Shared)) : nullptr;
+  row.sh = reinterpret_cast<Shared<T> *>(smem_raw);
+  row.bounds = p.bounds ? reinterpret_cast<uint16_t *>(smem_raw + sizeof(Shared<T>)) : nullptr;
   row.warp = threadIdx.x >> 5;
   row.lane = threadIdx.x & 31;
   row.blocks = 1 << p.log_blocks;
@@ -953,6 +1208,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
   row.first = row.warp * each_warp;
   row.mine = max(0, min(each_warp, row.segs - row.first));
   row.turn = 0;
+  row.log_q = 0;
+  while (((each_warp + (1 << row.log_q) - 1) >> row.log_q) > kParts) ++row.log_q;
 
   // the row's settings
   double temperature = p.temperature_rows ? (double)p.temperature_rows[t] : p.temperature;
@@ -967,8 +1224,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
   const bool top_k_one = top_k == 1;
   row.inv_t = 1.0 / temperature;
   row.c = (float)(1.4426950408889634 * row.inv_t);
+  row.c_rest = (float)(1.4426950408889634 * row.inv_t - (double)row.c);
 
   if (threadIdx.x < kTable) row.sh->table[threadIdx.x] = exp2((double)threadIdx.x / kTable);
+  __syncthreads();
   double rest;
   int masked;
   row.stats(rest, masked);
@@ -979,42 +1238,56 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
     row.cut_v = rho > 0.0 ? fmaxf(kLowest, __double2float_ru((double)row.m + temperature * log(rho))) : kLowest;
     row.cut_i = kNoIndex;
     if (top_k_one) {
-      id = row.first_of_max();
+      typename Row<T>::Pass a = row.of_kept(row.m);
+      a.split = -kNegInf;
+      a.rest = Row<T>::kFirst;
+      id = row.sum(a).n;
       count = 1;
     } else {
-      const auto kept = [&](float x, int i) { return row.kept(x, i); };
       bool whole = row.cut_v == kLowest;  // nothing is cut: the sums of the first sweep are those of what is kept
-      bool have = false;                  // the sums of what is kept lie in `chunk`
-      if (top_k > 0 && top_k < p.V - masked) {
-        row.template select<false>(1.0, (double)top_k, 0.0, row.floor_of(top_k), 0.0, count);
-        whole = false;
-      }
-      if (top_p < 1.0) {
-        const double all = whole ? rest + 1.0 : row.sum_of(row.cut_v, kept, count), unsure = whole ? row.eps() * all : 0.0;
-        // logits whose weight is under a V-th of 0.03 (1 - top_p) of the whole hold less than that much together
-        const double below = 0.03 * (1.0 - top_p) * all;
-        const float floor = __double2float_rd((double)row.m + temperature * log(below / (double)p.V));
-        have = row.template select<true>(top_p, all, unsure, fmaxf(row.cut_v, floor), below * 1.001, count);
-        whole = false;
-      }
-      double all;
-      if (whole) {
-        // by the warps' float32 sums, unless the border is too near for them
-        int n;
-        all = row.sum_of_row(0, n);
-        id = row.template find<true>((double)u * all, kept, 2.0 * row.eps() * all);
-        count = (int)p.V - masked;
-      }
-      if (!whole || id == kNoIndex) {
-        if (have) {
-          int n;
-          all = row.sum_of_row(0, n);
+#pragma unroll 1
+      for (int step = 0; step < 2; ++step) {  // top_k, then top_p
+        const bool weights = step == 1;
+        if (weights ? !(top_p < 1.0) : !(top_k > 0 && top_k < p.V - masked)) continue;
+        double share = 1.0, all = (double)top_k, unsure = 0.0, below = 0.0;
+        float floor;
+        if (weights) {
+          share = top_p;
+          all = rest + 1.0;
+          if (whole)
+            unsure = row.eps(all) * all;
+          else
+            all = row.sum(row.of_kept(kLowest)).all;
+          // logits whose weight is under a V-th of 0.03 (1 - top_p) of the whole hold less than that much together
+          below = 0.003 * (1.0 - top_p) * all;
+          floor = fmaxf(row.cut_v, __double2float_rd((double)row.m + temperature * log(below / (double)p.V)));
+          below *= 1.001;
         } else {
-          all = row.sum_of(row.cut_v, kept, count);
+          floor = row.floor_of(top_k);
         }
-        id = row.template find<true>((double)u * all, kept);
+        row.select(weights, share, all, unsure, floor, below);
+        whole = false;
       }
-      kept_rest = whole ? rest : all - 1.0;
+      // by the warps' float32 sums where nothing is cut, unless the border is too near for them
+      double all;
+      id = kNoIndex;
+      const bool was_whole = whole;
+#pragma unroll 1
+      while (id == kNoIndex) {
+        double unsure = 0.0;
+        if (whole) {
+          all = row.sum_of_chunks();
+          unsure = 2.0 * row.eps(all) * all;
+          count = (int)p.V - masked;
+        } else {
+          const typename Row<T>::Sum r = row.sum(row.of_kept(kLowest));
+          all = r.all;
+          count = r.n;
+        }
+        id = row.found(row.of_kept(kLowest), (double)u * all, unsure, false, whole);
+        whole = false;
+      }
+      kept_rest = was_whole ? rest : all - 1.0;
     }
   }
   // the block that has the token writes
@@ -1025,8 +1298,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
       static_cast<long long *>(p.ids)[t] = id;
     const float nan = __int_as_float(0x7fc00000);
     const double x = id >= 0 ? ((double)Storage<T>::widen(row.z[id]) - (double)row.m) * row.inv_t : 0.0;
-    if (p.logp) p.logp[t] = id >= 0 ? (float)(x - log1p(rest)) : nan;
-    if (p.logp_mp) p.logp_mp[t] = id >= 0 ? (float)(x - log1p(kept_rest)) : nan;
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+      float *to = side ? p.logp_mp : p.logp;
+      if (to) to[t] = id >= 0 ? (float)(x - log1p(side ? kept_rest : rest)) : nan;
+    }
     if (p.count) p.count[t] = count;
   }
   if (row.blocks > 1) row.meet();  // nobody leaves while its shared memory is read
@@ -1053,9 +1329,9 @@ cudaError_t launch(const dvp_sample_args *a, Params p, cudaStream_t stream) {
   const long long per = 32 / sizeof(T), segs = ((per - 1 + a->V + per - 1) / per + 31) / 32;
   const long long granules = (segs + blocks - 1) / blocks * 32;
   p.bounds = granules <= kMostBounds ? (int)granules : 0;
-  const size_t smem = sizeof(Shared) + (size_t)p.bounds * 2;
+  const size_t smem = sizeof(Shared<T>) + (size_t)p.bounds * 2;
   auto kernel = sample_kernel<T>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared) + kMostBounds * 2));
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared<T>) + kMostBounds * 2));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a->T << p.log_blocks), 1, 1);
