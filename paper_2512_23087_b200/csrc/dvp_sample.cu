@@ -26,7 +26,7 @@
 namespace dvp {
 namespace sample {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kList = 2048;
 constexpr int kTable = 64;
 constexpr int kParts = 128;         // sums that a warp keeps of its part of the row, of one piece or several each
@@ -177,8 +177,7 @@ template <typename T>
 struct Row {
   static constexpr int kPer = 32 / sizeof(T);  // logits of a granule
   using Shared = sample::Shared<T>;
-  Shared *sh;
-  uint16_t *bounds;  // bfloat16, rounded up; NULL: none
+  bool bounded;  // the granules' maxima are held
   const T *z;
   int V, off;                    // off: logits of the first granule that lie in front of the row
   int seg0, segs, all_segs;      // the block's pieces of 32 granules, the row's
@@ -193,6 +192,15 @@ struct Row {
   float cut_v;
   int cut_i;
 
+  // The block's shared memory, by its own name wherever it is used: through a pointer that is handed on, every access would be one of
+  // the general kind.
+  __device__ __forceinline__ static Shared *sh() {
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    return reinterpret_cast<Shared *>(smem_raw);
+  }
+  // The granules' maxima: bfloat16, rounded up.
+  __device__ __forceinline__ static uint16_t *bounds() { return reinterpret_cast<uint16_t *>(sh() + 1); }
+
   __device__ __forceinline__ void meet() const {
     if (blocks > 1) {
       __syncwarp();
@@ -203,15 +211,15 @@ struct Row {
     }
   }
   __device__ __forceinline__ const Shared *of(int r) const {
-    return static_cast<const Shared *>(__cluster_map_shared_rank(sh, (unsigned)r));
+    return static_cast<const Shared *>(__cluster_map_shared_rank(sh(), (unsigned)r));
   }
   // Every block's value to all of them.  Two slots in turn: whoever writes one again has met the others since they read it.
   __device__ __forceinline__ void tell(double a, float m_, int i) {
     turn ^= 1;
-    if (threadIdx.x == 0) sh->slot[turn] = Slot{a, m_, i};
+    if (threadIdx.x == 0) sh()->slot[turn] = Slot{a, m_, i};
     meet();
   }
-  __device__ __forceinline__ Slot told(int r) const { return r == rank ? sh->slot[turn] : of(r)->slot[turn]; }
+  __device__ __forceinline__ Slot told(int r) const { return r == rank ? sh()->slot[turn] : of(r)->slot[turn]; }
 
   __device__ __forceinline__ int first_of(int seg) const { return ((seg0 + seg) * 32 + lane) * kPer - off; }
   // A lane's granule of a piece; what lies outside the row is -inf.
@@ -239,7 +247,7 @@ struct Row {
     e = fma(e, r, 1.0 / 6.0);
     e = fma(e, r, 0.5);
     e = fma(e, r, 1.0);
-    const double q = sh->table[k & (kTable - 1)];
+    const double q = sh()->table[k & (kTable - 1)];
     e = fma(e * r, q, q);
     const double w = __hiloint2double(__double2hiint(e) + (k >> 6) * (1 << 20), __double2loint(e));
     return y > -700.0 ? w : 0.0;
@@ -260,7 +268,7 @@ struct Row {
     double s = 0.0;
     int gone = 0;                          // logits of -inf
     float of_part = 0.f;                   // the part's terms so far
-    double *parts = sh->part[warp];
+    double *parts = sh()->part[warp];
     constexpr int U = 2;
     uint32_t next[U][8];
 #pragma unroll
@@ -277,9 +285,9 @@ struct Row {
         float hi, lo;
         extremes(w, hi, lo);
         if (i0 + u + U < mine) load(seg + U, next[u]);
-        if (bounds) {
+        if (bounded) {
           const uint32_t b = __float_as_uint(hi);
-          bounds[seg * 32 + lane] = (uint16_t)(((b & 0x80000000u) ? b : b + 0xffffu) >> 16);
+          bounds()[seg * 32 + lane] = (uint16_t)(((b & 0x80000000u) ? b : b + 0xffffu) >> 16);
         }
         if (__any_sync(0xffffffffu, lo == kNegInf)) {
 #pragma unroll
@@ -334,14 +342,14 @@ struct Row {
   __device__ void stats(double &rest, int &masked) {
     const First f = first_sweep(*this);
     if (lane == 0) {
-      sh->warp_m[warp] = f.tm;
-      sh->warp_a[warp] = f.s;
-      sh->warp_b[warp] = f.n;
-      sh->warp_n[warp] = (uint32_t)f.gone;
+      sh()->warp_m[warp] = f.tm;
+      sh()->warp_a[warp] = f.s;
+      sh()->warp_b[warp] = f.n;
+      sh()->warp_n[warp] = (uint32_t)f.gone;
     }
     __syncthreads();
-    combine(kWarps, sh->warp_m[lane & (kWarps - 1)], sh->warp_a[lane & (kWarps - 1)], sh->warp_b[lane & (kWarps - 1)], m, rest);
-    masked = __reduce_add_sync(0xffffffffu, lane < kWarps ? (int)sh->warp_n[lane & (kWarps - 1)] : 0);
+    combine(kWarps, sh()->warp_m[lane & (kWarps - 1)], sh()->warp_a[lane & (kWarps - 1)], sh()->warp_b[lane & (kWarps - 1)], m, rest);
+    masked = __reduce_add_sync(0xffffffffu, lane < kWarps ? (int)sh()->warp_n[lane & (kWarps - 1)] : 0);
     if (blocks > 1) {
       tell(rest, m, masked);
       const Slot o = told(lane & (blocks - 1));
@@ -350,9 +358,9 @@ struct Row {
     }
     masked -= all_segs * 32 * kPer - V;  // what lies outside the row
     if (threadIdx.x < kWarps) {
-      const float mi = sh->warp_m[threadIdx.x];
-      sh->chunk[threadIdx.x] =
-          mi > kNegInf ? (sh->warp_a[threadIdx.x] + sh->warp_b[threadIdx.x]) * power(((double)mi - (double)m) * inv_t) : 0.0;
+      const float mi = sh()->warp_m[threadIdx.x];
+      sh()->chunk[threadIdx.x] =
+          mi > kNegInf ? (sh()->warp_a[threadIdx.x] + sh()->warp_b[threadIdx.x]) * power(((double)mi - (double)m) * inv_t) : 0.0;
     }
     __syncthreads();
   }
@@ -468,15 +476,14 @@ struct Row {
   // each lane by itself would form exponentials for one or two lanes at a time.  Leaves the warps' sums in `chunk` and tells the
   // blocks theirs; the order of the additions is fixed.
   __device__ __noinline__ static Sum pass(Row row, const Pass a) {
-    Shared *sh = row.sh;
-    float *value = sh->compact.value[row.warp];
-    uint16_t *place = sh->compact.place[row.warp];
+    float *value = sh()->compact.value[row.warp];
+    uint16_t *place = sh()->compact.place[row.warp];
     double acc = 0.0, of_part = 0.0;
-    double *parts = sh->part[row.warp];
+    double *parts = sh()->part[row.warp];
     int n = 0, best = kNoIndex;
     const auto hot = [&](int i) {
       return i < row.mine &&
-             (!row.bounds || __uint_as_float((uint32_t)row.bounds[(row.first + i) * 32 + row.lane] << 16) >= a.v);
+             (!row.bounded || __uint_as_float((uint32_t)bounds()[(row.first + i) * 32 + row.lane] << 16) >= a.v);
     };
     const bool plain = a.i == kNoIndex && a.most == -kNegInf;
     uint32_t next[8];
@@ -562,7 +569,7 @@ struct Row {
             if (a.rest == kFirst) {
               best = min(best, at_row);
             } else if (a.rest == kBinsOfKeys) {
-              atomicAdd(&sh->hist[(a.k_hi - key_of(v)) >> a.shift], 1u);
+              atomicAdd(&sh()->hist[(a.k_hi - key_of(v)) >> a.shift], 1u);
             } else if (a.rest == kToList) {
               row.to_list(v, at_row);
             }
@@ -581,18 +588,18 @@ struct Row {
     n = first ? __reduce_min_sync(0xffffffffu, best) : __reduce_add_sync(0xffffffffu, n);
     __syncthreads();  // chunk and warp_n have been read
     if (row.lane == 0) {
-      sh->chunk[row.warp] = acc;
-      sh->warp_n[row.warp] = (uint32_t)n;
+      sh()->chunk[row.warp] = acc;
+      sh()->warp_n[row.warp] = (uint32_t)n;
     }
     __syncthreads();
-    const int ns = (int)sh->warp_n[row.lane & (kWarps - 1)];
+    const int ns = (int)sh()->warp_n[row.lane & (kWarps - 1)];
     n = first ? __reduce_min_sync(0xffffffffu, ns) : __reduce_add_sync(0xffffffffu, row.lane < kWarps ? ns : 0);
     Sum r;
-    r.all = warp_sum(row.lane < kWarps ? sh->chunk[row.lane & (kWarps - 1)] : 0.0);
+    r.all = warp_sum(row.lane < kWarps ? sh()->chunk[row.lane & (kWarps - 1)] : 0.0);
     r.n = n;
     if (row.blocks > 1) {
       row.turn ^= 1;
-      if (threadIdx.x == 0) sh->slot[row.turn] = Slot{r.all, 0.f, n};
+      if (threadIdx.x == 0) sh()->slot[row.turn] = Slot{r.all, 0.f, n};
       row.meet();
       const Slot o = row.told(row.lane & (row.blocks - 1));
       r.all = warp_sum(row.lane < row.blocks ? o.a : 0.0);
@@ -607,9 +614,9 @@ struct Row {
   }
   // The histogram of the distances of what is kept, none below `low`: most of a row's logits, one by one.
   __device__ __noinline__ static void bins_of_distance(Row row, float low, float per) {
-    uint32_t *hist = row.sh->hist;
+    uint32_t *hist = row.sh()->hist;
     const auto hot = [&](int i) {
-      return i < row.mine && (!row.bounds || __uint_as_float((uint32_t)row.bounds[(row.first + i) * 32 + row.lane] << 16) >= low);
+      return i < row.mine && (!row.bounded || __uint_as_float((uint32_t)bounds()[(row.first + i) * 32 + row.lane] << 16) >= low);
     };
     const bool plain = low > row.cut_v || row.cut_i == kNoIndex;
     const float v = fmaxf(low, row.cut_v);
@@ -637,7 +644,7 @@ struct Row {
   }
   // The sum of the warps' parts that lie in `chunk`.
   __device__ __forceinline__ double sum_of_chunks() {
-    double v = warp_sum(lane < kWarps ? sh->chunk[lane & (kWarps - 1)] : 0.0);
+    double v = warp_sum(lane < kWarps ? sh()->chunk[lane & (kWarps - 1)] : 0.0);
     if (blocks > 1) {
       tell(v, 0.f, 0);
       v = warp_sum(lane < blocks ? told(lane & (blocks - 1)).a : 0.0);
@@ -652,7 +659,6 @@ struct Row {
   // Known to the block that has it alone; the others get -2.  `unsure`: how far the parts may be off; then the answer is
   // kNoIndex where that matters, known to all.
   __device__ __noinline__ static int find(Row row, const Pass a, double aim, double unsure, bool pairs) {
-    Shared *sh = row.sh;
     const int lane = row.lane, blocks = row.blocks;
     const auto amount = [&](float x, int i) {
       if (!(x >= a.v && x <= a.most && (x > a.v || i <= a.i))) return 0.0;
@@ -674,13 +680,13 @@ struct Row {
     int at = -2;
     if (owner == row.rank) {
       // the warp whose part it is
-      const int of_warp = max(0, passes(lane < kWarps ? sh->chunk[lane & (kWarps - 1)] : 0.0, run));
+      const int of_warp = max(0, passes(lane < kWarps ? sh()->chunk[lane & (kWarps - 1)] : 0.0, run));
       const int per = (row.segs + kWarps - 1) / kWarps, s0 = of_warp * per, s1 = min(row.segs, s0 + per);
       // its parts, every warp alike
       int part_of = 0, piece = -1;
       {
         const int parts = (s1 - s0 + (1 << row.log_q) - 1) >> row.log_q;
-        const double *stored = sh->part[of_warp];
+        const double *stored = sh()->part[of_warp];
         double run_last = run;
 #pragma unroll 1
         for (int q = 0; q < parts && piece < 0; q += 32) {
@@ -735,10 +741,10 @@ struct Row {
 #pragma unroll 1
       for (int g = row.warp; g < kPer; g += kWarps) {
         const double all = warp_sum(term(g));
-        if (lane == 0) sh->group[g] = all;
+        if (lane == 0) sh()->group[g] = all;
       }
       __syncthreads();
-      const int group = max(0, passes(lane < kPer ? sh->group[lane] : 0.0, run));
+      const int group = max(0, passes(lane < kPer ? sh()->group[lane] : 0.0, run));
       clear = clear && hit;
       const double g = term(group);
       const int who = max(0, passes(g, run));
@@ -769,10 +775,10 @@ struct Row {
   __device__ float floor_of(long long k) {
     float low = cut_v;
     const int n = segs * 16;  // pairs
-    if (bounds && k <= 2 * n) {
-      if (threadIdx.x < 3) sh->counter[threadIdx.x] = 0;
+    if (bounded && k <= 2 * n) {
+      if (threadIdx.x < 3) sh()->counter[threadIdx.x] = 0;
       __syncthreads();
-      const uint32_t *pairs = reinterpret_cast<const uint32_t *>(bounds);
+      const uint32_t *pairs = reinterpret_cast<const uint32_t *>(bounds());
       uint32_t lo = 0, hi = 0xffff;  // of the order: the largest b that k bounds reach
       for (int round = 0; lo < hi; ++round) {
         const uint32_t mid = (lo + hi + 1) >> 1;
@@ -785,10 +791,10 @@ struct Row {
         }
         reach = __reduce_add_sync(0xffffffffu, reach);
         // three counters in turn: one is added to, one is read, one is cleared for the next
-        if (lane == 0 && reach) atomicAdd(&sh->counter[round % 3], (uint32_t)reach);
-        if (threadIdx.x == 0) sh->counter[(round + 1) % 3] = 0;
+        if (lane == 0 && reach) atomicAdd(&sh()->counter[round % 3], (uint32_t)reach);
+        if (threadIdx.x == 0) sh()->counter[(round + 1) % 3] = 0;
         __syncthreads();
-        if ((long long)sh->counter[round % 3] >= k)
+        if ((long long)sh()->counter[round % 3] >= k)
           lo = mid;
         else
           hi = mid - 1;
@@ -829,8 +835,8 @@ struct Row {
         unsure = 0.0;
       }
       __syncthreads();
-      for (int i = threadIdx.x; i < kBins; i += kThreads) sh->hist[i] = 0;
-      if (threadIdx.x == 0) sh->list_n = 0;
+      for (int i = threadIdx.x; i < kBins; i += kThreads) sh()->hist[i] = 0;
+      if (threadIdx.x == 0) sh()->list_n = 0;
       __syncthreads();
       Pass a = of_kept(low);
       a.weights = weights;
@@ -874,10 +880,10 @@ struct Row {
         int n = 0;
 #pragma unroll 1
         for (int r = 0; r < blocks; ++r) {
-          const Shared *o = r == rank ? sh : of(r);
+          const Shared *o = r == rank ? sh() : of(r);
           const int k = (int)o->list_n;
           if (n + k <= kList)
-            for (int i = threadIdx.x; i < k; i += kThreads) sh->sorted[n + i] = o->list[i];
+            for (int i = threadIdx.x; i < k; i += kThreads) sh()->sorted[n + i] = o->list[i];
           n += k;
         }
         if (blocks > 1) meet();  // the lists have been read
@@ -892,14 +898,14 @@ struct Row {
           // errors are the smaller by 1 - share; mostly nothing lies so near the border that they matter.
           const double end = (1.0 - share) * all;
           if (!cut_from_list(true, n, tail - end, true, (1.0 - share) * unsure + tail * eps(tail), last)) {
-            for (int i = threadIdx.x; i < n; i += kThreads) sh->list[i] = sh->sorted[i];  // passes take their place
+            for (int i = threadIdx.x; i < n; i += kThreads) sh()->list[i] = sh()->sorted[i];  // passes take their place
             __syncthreads();
             aim = share * whole();
             a.v = high;
             a.i = -1;
             a.rest = kNone;
             above = sum(a);
-            for (int i = threadIdx.x; i < n; i += kThreads) sh->sorted[i] = sh->list[i];
+            for (int i = threadIdx.x; i < n; i += kThreads) sh()->sorted[i] = sh()->list[i];
             __syncthreads();
             cut_from_list(true, n, aim - above.all, false, 0.0, last);
           }
@@ -910,8 +916,8 @@ struct Row {
         return;
       }
       bracket(weights, level, aim, above.all, all, share * unsure, below, unsure, per, k_lo, k_hi, shift);
-      const uint32_t lo = sh->pick_lo, hi = sh->pick_hi;
-      n_in = sh->pick_last;
+      const uint32_t lo = sh()->pick_lo, hi = sh()->pick_hi;
+      n_in = sh()->pick_last;
       meet();  // the histograms have been read
       if (n_in == 0) return;  // less than the aim in all: everything stays
       if (level == 0) {
@@ -928,13 +934,13 @@ struct Row {
     }
   }
   __device__ __forceinline__ void set_cut(int last) {
-    const uint64_t item = sh->sorted[last];
+    const uint64_t item = sh()->sorted[last];
     cut_v = value_of(~(uint32_t)(item >> 32));
     cut_i = (int)(uint32_t)item;
   }
   __device__ __forceinline__ void to_list(float x, int i) const {
-    const uint32_t to = atomicAdd(&sh->list_n, 1u);
-    if (to < kList) sh->list[to] = (uint64_t)(~key_of(x)) << 32 | (uint32_t)i;
+    const uint32_t to = atomicAdd(&sh()->list_n, 1u);
+    if (to < kList) sh()->list[to] = (uint64_t)(~key_of(x)) << 32 | (uint32_t)i;
   }
   // Of a row that nothing is cut from: the float32 sum of the weights of logits below `low`, with what lies from there to `high` to
   // the list.  Leaves `chunk` alone.
@@ -973,9 +979,9 @@ struct Row {
   __device__ double behind(float low, float high) {
     const double ws = behind_of_warp(*this, low, high);
     __syncthreads();
-    if (lane == 0) sh->warp_a[warp] = ws;
+    if (lane == 0) sh()->warp_a[warp] = ws;
     __syncthreads();
-    double own = warp_sum(lane < kWarps ? sh->warp_a[lane & (kWarps - 1)] : 0.0);
+    double own = warp_sum(lane < kWarps ? sh()->warp_a[lane & (kWarps - 1)] : 0.0);
     if (blocks > 1) {
       tell(own, 0.f, 0);
       own = warp_sum(lane < blocks ? told(lane & (blocks - 1)).a : 0.0);
@@ -1002,7 +1008,7 @@ struct Row {
     for (int j = 0; j < kOwn; ++j) n[j] = 0;
 #pragma unroll 1
     for (int r = 0; r < blocks; ++r) {
-      const uint32_t *hist = (r ? of((rank + r) & (blocks - 1)) : sh)->hist + threadIdx.x * kOwn;
+      const uint32_t *hist = (r ? of((rank + r) & (blocks - 1)) : sh())->hist + threadIdx.x * kOwn;
 #pragma unroll
       for (int j = 0; j < kOwn; j += 4) {
         const uint4 q = *reinterpret_cast<const uint4 *>(hist + j);
@@ -1032,18 +1038,18 @@ struct Row {
     const double least_up = warp_scan(least_sum), most_up = warp_scan(most_sum);
     __syncthreads();
     if (lane == 31) {
-      sh->warp_a[warp] = least_up;
-      sh->warp_b[warp] = most_up;
+      sh()->warp_a[warp] = least_up;
+      sh()->warp_b[warp] = most_up;
     }
     if (threadIdx.x == 0) {
-      sh->pick_lo = kBins;   // the first bin up to which there can be as much as the aim
-      sh->pick_hi = kBins;   // the first up to which there is
-      sh->pick_last = 0;     // the last that holds anything
+      sh()->pick_lo = kBins;   // the first bin up to which there can be as much as the aim
+      sh()->pick_hi = kBins;   // the first up to which there is
+      sh()->pick_last = 0;     // the last that holds anything
     }
     __syncthreads();
     // the warps in front of this one, and all
-    const double la = warp_scan(lane < kWarps ? sh->warp_a[lane & (kWarps - 1)] : 0.0);
-    const double lb = warp_scan(lane < kWarps ? sh->warp_b[lane & (kWarps - 1)] : 0.0);
+    const double la = warp_scan(lane < kWarps ? sh()->warp_a[lane & (kWarps - 1)] : 0.0);
+    const double lb = warp_scan(lane < kWarps ? sh()->warp_b[lane & (kWarps - 1)] : 0.0);
     const double a_before = __shfl_sync(0xffffffffu, la, max(warp - 1, 0)), b_before = __shfl_sync(0xffffffffu, lb, max(warp - 1, 0));
     double least_run = above + (warp ? a_before : 0.0) + (least_up - least_sum);
     double most_run = above + (warp ? b_before : 0.0) + (most_up - most_sum);
@@ -1071,13 +1077,13 @@ struct Row {
     first_hi = __reduce_min_sync(0xffffffffu, first_hi);
     last_any = __reduce_max_sync(0xffffffffu, last_any);
     if (lane == 0) {
-      if (first_lo < (uint32_t)kBins) atomicMin(&sh->pick_lo, first_lo);
-      if (first_hi < (uint32_t)kBins) atomicMin(&sh->pick_hi, first_hi);
-      if (last_any) atomicMax(&sh->pick_last, last_any);
+      if (first_lo < (uint32_t)kBins) atomicMin(&sh()->pick_lo, first_lo);
+      if (first_hi < (uint32_t)kBins) atomicMin(&sh()->pick_hi, first_hi);
+      if (last_any) atomicMax(&sh()->pick_last, last_any);
     }
     __syncthreads();
-    uint32_t lo = sh->pick_lo, hi = min(sh->pick_hi, (uint32_t)kBins - 1);
-    if (level > 0 && lo == kBins) lo = hi = sh->pick_last;  // the cut is in the bracket: what is missing is a rounding
+    uint32_t lo = sh()->pick_lo, hi = min(sh()->pick_hi, (uint32_t)kBins - 1);
+    if (level > 0 && lo == kBins) lo = hi = sh()->pick_last;  // the cut is in the bracket: what is missing is a rounding
     // logits in bins lo to hi
     uint32_t inside = 0;
 #pragma unroll
@@ -1088,12 +1094,12 @@ struct Row {
     inside = __reduce_add_sync(0xffffffffu, inside);
     __syncthreads();
     if (threadIdx.x == 0) {
-      sh->pick_lo = lo;
-      sh->pick_hi = hi;
-      sh->pick_last = 0;
+      sh()->pick_lo = lo;
+      sh()->pick_hi = hi;
+      sh()->pick_last = 0;
     }
     __syncthreads();
-    if (lane == 0 && inside) atomicAdd(&sh->pick_last, inside);
+    if (lane == 0 && inside) atomicAdd(&sh()->pick_last, inside);
     __syncthreads();
   }
 
@@ -1103,7 +1109,7 @@ struct Row {
     if (n <= kThreads) {
       // an item a thread; partners in the same warp are met by shuffles
       const int i = threadIdx.x;
-      uint64_t x = i < n ? sh->sorted[i] : ~0ull;
+      uint64_t x = i < n ? sh()->sorted[i] : ~0ull;
       int size = 32;
       while (size < n) size <<= 1;
       const bool in = (i & ~31) < size;
@@ -1114,9 +1120,9 @@ struct Row {
           uint64_t y;
           if (j >= 32) {
             __syncthreads();
-            if (in) sh->sorted[i] = x;
+            if (in) sh()->sorted[i] = x;
             __syncthreads();
-            y = in ? sh->sorted[i ^ j] : x;
+            y = in ? sh()->sorted[i ^ j] : x;
           } else {
             y = __shfl_xor_sync(0xffffffffu, x, j);
           }
@@ -1124,13 +1130,13 @@ struct Row {
           if ((low == rising) ? y < x : y > x) x = y;
         }
       __syncthreads();
-      if (in) sh->sorted[i] = x;
+      if (in) sh()->sorted[i] = x;
       __syncthreads();
       return;
     }
     int size = 32;
     while (size < n) size <<= 1;
-    for (int i = n + threadIdx.x; i < size; i += kThreads) sh->sorted[i] = ~0ull;
+    for (int i = n + threadIdx.x; i < size; i += kThreads) sh()->sorted[i] = ~0ull;
     __syncthreads();
 #pragma unroll 1
     for (int k = 2; k <= size; k <<= 1)
@@ -1139,10 +1145,10 @@ struct Row {
 #pragma unroll 1
         for (int t = threadIdx.x; t < size / 2; t += kThreads) {
           const int a = (t & ~(j - 1)) * 2 + (t & (j - 1)), b = a + j;
-          const uint64_t x = sh->sorted[a], y = sh->sorted[b];
+          const uint64_t x = sh()->sorted[a], y = sh()->sorted[b];
           if ((x > y) == ((a & k) == 0)) {
-            sh->sorted[a] = y;
-            sh->sorted[b] = x;
+            sh()->sorted[a] = y;
+            sh()->sorted[b] = x;
           }
         }
         __syncthreads();
@@ -1156,14 +1162,14 @@ struct Row {
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const int i = threadIdx.x * kOwn + j;
-      w[j] = i < n ? weights ? weight(value_of(~(uint32_t)(sh->sorted[i] >> 32))) : 1.0 : 0.0;
+      w[j] = i < n ? weights ? weight(value_of(~(uint32_t)(sh()->sorted[i] >> 32))) : 1.0 : 0.0;
       sum += w[j];
     }
     const double up_to = warp_scan(sum);
     __syncthreads();
-    if (lane == 31) sh->warp_a[warp] = up_to;
+    if (lane == 31) sh()->warp_a[warp] = up_to;
     __syncthreads();
-    const double la = warp_scan(lane < kWarps ? sh->warp_a[lane & (kWarps - 1)] : 0.0), before = __shfl_sync(0xffffffffu, la, max(warp - 1, 0));
+    const double la = warp_scan(lane < kWarps ? sh()->warp_a[lane & (kWarps - 1)] : 0.0), before = __shfl_sync(0xffffffffu, la, max(warp - 1, 0));
     double run = (warp ? before : 0.0) + (up_to - sum);
     if (from_end) aim += __shfl_sync(0xffffffffu, la, 31);
     int in_front = 0, unclear = 0;  // of the list, before which less than the aim lies: its front
@@ -1177,20 +1183,18 @@ struct Row {
       unclear |= unsure > 0.0 && i == n - 1 && run - aim <= unsure;
     }
     in_front = __reduce_add_sync(0xffffffffu, in_front);
-    if (lane == 0) sh->warp_n[warp] = (uint32_t)in_front;
+    if (lane == 0) sh()->warp_n[warp] = (uint32_t)in_front;
     unclear = __syncthreads_or(unclear);
-    last = (int)__reduce_add_sync(0xffffffffu, lane < kWarps ? sh->warp_n[lane & (kWarps - 1)] : 0u) - 1;
+    last = (int)__reduce_add_sync(0xffffffffu, lane < kWarps ? sh()->warp_n[lane & (kWarps - 1)] : 0u) - 1;
     __syncthreads();  // warp_n and warp_a have been read
     return !unclear;
   }
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Params p) {
-  extern __shared__ __align__(16) uint8_t smem_raw[];
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
   Row<T> row;
-  row.sh = reinterpret_cast<Shared<T> *>(smem_raw);
-  row.bounds = p.bounds ? reinterpret_cast<uint16_t *>(smem_raw + sizeof(Shared<T>)) : nullptr;
+  row.bounded = p.bounds != 0;
   row.warp = threadIdx.x >> 5;
   row.lane = threadIdx.x & 31;
   row.blocks = 1 << p.log_blocks;
@@ -1226,7 +1230,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const Params p) {
   row.c = (float)(1.4426950408889634 * row.inv_t);
   row.c_rest = (float)(1.4426950408889634 * row.inv_t - (double)row.c);
 
-  if (threadIdx.x < kTable) row.sh->table[threadIdx.x] = exp2((double)threadIdx.x / kTable);
+  if (threadIdx.x < kTable) row.sh()->table[threadIdx.x] = exp2((double)threadIdx.x / kTable);
   __syncthreads();
   double rest;
   int masked;
