@@ -35,7 +35,6 @@ EXPORTS = ("dvp_forward", "dvp_backward", "dvp_fused_lmhead_forward_backward",
            "dvp_quantize_fp8", "dvp_gemm_fp8", "dvp_sample")
 
 _DTYPES = {torch.float32: DVP_F32, torch.bfloat16: DVP_BF16, torch.float16: DVP_F16}
-_OUT_DTYPES = {**_DTYPES, torch.float8_e4m3fn: DVP_E4M3}
 FP8_BLOCK = 128   # columns, and rows of a weight, that share a scale
 _SIDE_FIELDS = ("max", "lse", "lse_safe", "logp", "logp_mp", "comp_mp", "count", "mask", "log_cov")
 
@@ -312,15 +311,8 @@ _BACKWARD_PACK = struct.Struct("=I3i4qd9QIIfI")
 _MONITOR_PACK = struct.Struct("=Ii4q7Q")
 _SEQUENCE_PACK = struct.Struct("=II2q2Qd9Q")
 _FUSED_PACK = struct.Struct("=Ii8qd7Qii18Q5QIff4xQ")
-_RMS_NORM_PACK = struct.Struct("=I3i7qd8Q")
-_RMS_NORM_BACKWARD_PACK = struct.Struct("=I3i6q10QiI")
 _QUANTIZE_FP8_PACK = struct.Struct("=Ii5q4QiI")
-_GEMM_FP8_PACK = struct.Struct("=Ii8q7QII")
-_SAMPLE_PACK = struct.Struct("=I2iI3q2Q3dq9Q")
-assert _SAMPLE_PACK.size == ctypes.sizeof(SampleArgs)
-assert _QUANTIZE_FP8_PACK.size == ctypes.sizeof(QuantizeFp8Args) and _GEMM_FP8_PACK.size == ctypes.sizeof(GemmFp8Args)
-assert _RMS_NORM_PACK.size == ctypes.sizeof(RmsNormArgs)
-assert _RMS_NORM_BACKWARD_PACK.size == ctypes.sizeof(RmsNormBackwardArgs)
+assert _QUANTIZE_FP8_PACK.size == ctypes.sizeof(QuantizeFp8Args)
 assert _FUSED_PACK.size == ctypes.sizeof(FusedArgs)
 assert _FORWARD_PACK.size == ctypes.sizeof(ForwardArgs) and _BACKWARD_PACK.size == ctypes.sizeof(BackwardArgs)
 assert _MONITOR_PACK.size == ctypes.sizeof(MonitorArgs) and _SEQUENCE_PACK.size == ctypes.sizeof(SequenceArgs)
@@ -377,11 +369,12 @@ def load_library() -> ctypes.CDLL:
         lib.dvp_debug_bounds_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
         lib.dvp_debug_bounds_status.restype = ctypes.c_int
         lib.packed = {}   # the entry points that take a packed struct
-        for name in ("dvp_forward", "dvp_backward", "dvp_monitor", "dvp_sequence_aggregate", "dvp_rms_norm",
-                     "dvp_rms_norm_backward", "dvp_quantize_fp8", "dvp_gemm_fp8", "dvp_sample"):
+        for name in ("dvp_forward", "dvp_backward", "dvp_monitor", "dvp_sequence_aggregate", "dvp_quantize_fp8"):
             fn = lib[name]   # a function object of its own, with its own argtypes
             fn.argtypes, fn.restype = [ctypes.c_char_p], ctypes.c_int
             lib.packed[name] = fn
+        lib.at = {name: ctypes.cast(lib[name], ctypes.c_void_p).value
+                  for name in ("dvp_rms_norm", "dvp_rms_norm_backward", "dvp_gemm_fp8", "dvp_sample", "dvp_workspace_bytes")}
         lib.forward_at = ctypes.cast(lib.dvp_forward, ctypes.c_void_p).value
         _lib = lib
     return _lib
@@ -434,6 +427,11 @@ def _stream(stream) -> int:
     return stream.cuda_stream
 
 
+def _raw(stream):
+    """A stream's address, None for the current one."""
+    return None if stream is None else stream.cuda_stream
+
+
 def _check_matrix(name: str, x: torch.Tensor):
     if x.dim() != 2 or x.stride(1) != 1:
         raise ValueError(f"{name} must be 2-D with unit inner stride")
@@ -484,30 +482,11 @@ def _int32(x) -> int:
     return (int(x) + 0x80000000 & 0xffffffff) - 0x80000000
 
 
-def _check_same_device(like: torch.Tensor, **others):
-    for name, t in others.items():
-        if t is not None and t.device != like.device:
-            raise ValueError(f"{name} must live on {like.device}")
-
-
 def _on_device_of(t: torch.Tensor):
     """The library launches on the current device: for the length of the block that is the tensor's."""
     if t.get_device() == torch.cuda.current_device():
         return contextlib.nullcontext()
     return torch.cuda.device(t.get_device())
-
-
-def _check_vector(name: str, x: torch.Tensor, n: int, dtypes):
-    if x.dim() != 1 or x.shape[0] != n or x.stride(0) != 1 and n > 1:
-        raise ValueError(f"{name} must be a contiguous vector of {n} elements")
-    if x.dtype not in dtypes:
-        raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}")
-
-
-def _check_like(name: str, x: torch.Tensor, shape, dtype):
-    _check_matrix(name, x)
-    if tuple(x.shape) != tuple(shape) or x.dtype != dtype:
-        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}")
 
 
 def _id_dtype(ids: torch.Tensor) -> int:
@@ -827,34 +806,11 @@ def dvp_rms_norm(x: torch.Tensor, weight: torch.Tensor, *, residual: torch.Tenso
     scale for each row and block of 128 columns, as ``dvp_gemm_fp8`` takes it.  Returns a namespace with ``y``, ``scale``
     [T, ceil(H / 128)] or None, ``residual`` (``x + residual`` in the type of ``x``, or None; written to ``residual_out``
     where that is given, which may be ``x`` or ``residual``) and ``rstd`` [T] float32 for ``dvp_rms_norm_backward``."""
-    packed = load_library().packed
-    _check_matrix("x", x)
-    T, H = x.shape
-    out_dtype = out_dtype or x.dtype
-    if x.dtype not in _DTYPES or out_dtype not in _OUT_DTYPES:
-        raise TypeError("x must be float32, bfloat16 or float16, out_dtype one of these or float8_e4m3fn")
-    _check_vector("weight", weight, H, (x.dtype, torch.float32))
-    _check_same_device(x, weight=weight, residual=residual, residual_out=residual_out)
-    if residual is not None:
-        _check_like("residual", residual, (T, H), x.dtype)
-        if residual_out is None:
-            residual_out = x.new_empty((T, H))
-    if residual_out is not None:
-        _check_like("residual_out", residual_out, (T, H), x.dtype)
-    fp8 = out_dtype == torch.float8_e4m3fn
-    # 8-bit rows start on 16-byte boundaries, where the tensor cores' loads want them
-    y = x.new_empty((T, -(-H // 16) * 16), dtype=out_dtype)[:, :H] if fp8 else x.new_empty((T, H), dtype=out_dtype)
-    scale = x.new_empty((T, -(-H // FP8_BLOCK)), dtype=torch.float32) if fp8 else None
-    rstd = x.new_empty(T, dtype=torch.float32)
-    with _on_device_of(x):
-        st = packed["dvp_rms_norm"](_RMS_NORM_PACK.pack(
-            _RMS_NORM_PACK.size, _DTYPES[x.dtype], _DTYPES[weight.dtype], _OUT_DTYPES[out_dtype], T, H, x.stride(0),
-            residual.stride(0) if residual is not None else 0, residual_out.stride(0) if residual_out is not None else 0,
-            y.stride(0), scale.stride(0) if fp8 else 0, float(eps), x.data_ptr(), _address(residual), weight.data_ptr(),
-            _address(residual_out), y.data_ptr(), _address(scale), rstd.data_ptr(), _stream(stream)))
-    if st != DVP_OK:
-        raise DvpError(st, "dvp_rms_norm")
-    return SimpleNamespace(y=y, scale=scale, residual=residual_out, rstd=rstd)
+    lib = load_library()
+    res = _host.rms_norm(lib.at["dvp_rms_norm"], x, weight, residual, float(eps), out_dtype, residual_out, _raw(stream))
+    if type(res) is int:
+        raise DvpError(res, "dvp_rms_norm")
+    return res
 
 
 def dvp_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, *,
@@ -866,37 +822,11 @@ def dvp_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tenso
     (in the type of ``h``; the gradient of ``x`` and of the residual) and ``d_weight`` [H] float32, added to the given one
     with ``accumulate_dw``."""
     lib = load_library()
-    _check_matrix("dy", dy)
-    _check_matrix("h", h)
-    T, H = h.shape
-    if dy.shape != h.shape:
-        raise ValueError("dy must match h in shape")
-    if h.dtype not in _DTYPES or dy.dtype not in _DTYPES:
-        raise TypeError("h and dy must be float32, bfloat16 or float16")
-    _check_vector("weight", weight, H, (h.dtype, torch.float32))
-    _check_vector("rstd", rstd, T, (torch.float32,))
-    _check_same_device(h, dy=dy, weight=weight, rstd=rstd, d_residual=d_residual, d_weight=d_weight, workspace=workspace)
-    if d_residual is not None:
-        _check_like("d_residual", d_residual, (T, H), h.dtype)
-    if d_weight is None:
-        if accumulate_dw:
-            raise ValueError("accumulate_dw needs d_weight")
-        d_weight = h.new_empty(H, dtype=torch.float32)
-    _check_vector("d_weight", d_weight, H, (torch.float32,))
-    d_x = h.new_empty((T, H))
-    fields = [_RMS_NORM_BACKWARD_PACK.size, _DTYPES[h.dtype], _DTYPES[weight.dtype], _DTYPES[dy.dtype], T, H, dy.stride(0),
-              h.stride(0), d_residual.stride(0) if d_residual is not None else 0, d_x.stride(0), dy.data_ptr(), h.data_ptr(),
-              weight.data_ptr(), rstd.data_ptr(), _address(d_residual), d_x.data_ptr(), d_weight.data_ptr(), 0, 0, 0,
-              int(bool(accumulate_dw)), 0]
-    if workspace is None:
-        need = lib.dvp_workspace_bytes(DVP_ENTRY_RMS_NORM_BACKWARD, _RMS_NORM_BACKWARD_PACK.pack(*fields))
-        workspace = h.new_empty(max(need, 256), dtype=torch.uint8)
-    with _on_device_of(h):
-        fields[17:20] = workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)
-        st = lib.packed["dvp_rms_norm_backward"](_RMS_NORM_BACKWARD_PACK.pack(*fields))
-    if st != DVP_OK:
-        raise DvpError(st, "dvp_rms_norm_backward")
-    return SimpleNamespace(d_x=d_x, d_weight=d_weight)
+    res = _host.rms_norm_backward(lib.at["dvp_rms_norm_backward"], lib.at["dvp_workspace_bytes"], dy, h, weight, rstd, d_residual,
+                                  d_weight, bool(accumulate_dw), workspace, _raw(stream))
+    if type(res) is int:
+        raise DvpError(res, "dvp_rms_norm_backward")
+    return res
 
 
 def dvp_quantize_fp8(x: torch.Tensor, *, block_rows: int = FP8_BLOCK, stream=None):
@@ -927,36 +857,11 @@ def dvp_gemm_fp8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scal
     16-byte boundaries, ``a_scale`` [M, ceil(K / 128)] and ``b_scale`` [ceil(N / 128), ceil(K / 128)] their float32 scales
     (``dvp_rms_norm``, ``dvp_quantize_fp8``).  Sums over a block of 128 are formed in the tensor cores and added up in
     float32; the result is rounded once, to ``out_dtype``.  Returns (out, status) as ``dvp_gemm_tn`` does."""
-    packed = load_library().packed
-    for name, x, dtype in (("a", a, torch.float8_e4m3fn), ("b", b, torch.float8_e4m3fn), ("a_scale", a_scale, torch.float32),
-                           ("b_scale", b_scale, torch.float32)):
-        _check_matrix(name, x)
-        if x.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype}")
-    (M, K), N = a.shape, b.shape[0]
-    if b.shape[1] != K:
-        raise ValueError("a and b must have the same number of columns")
-    blocks = -(-K // FP8_BLOCK)
-    if a_scale.shape != (M, blocks) or b_scale.shape != (-(-N // FP8_BLOCK), blocks):
-        raise ValueError("a_scale must be [M, ceil(K / 128)] and b_scale [ceil(N / 128), ceil(K / 128)]")
-    if out is None:
-        out = a.new_empty((M, N), dtype=out_dtype)
-    else:
-        _check_matrix("out", out)
-        if out.shape != (M, N):
-            raise ValueError(f"out must be {(M, N)}")
-    if out.dtype not in _DTYPES:
-        raise TypeError("out must be float32, bfloat16 or float16")
-    _check_same_device(a, a_scale=a_scale, b=b, b_scale=b_scale, out=out)
-    status = a.new_empty(1, dtype=torch.int32) if M and N else a.new_zeros(1, dtype=torch.int32)
-    with _on_device_of(a):
-        st = packed["dvp_gemm_fp8"](_GEMM_FP8_PACK.pack(
-            _GEMM_FP8_PACK.size, _DTYPES[out.dtype], M, N, K, a.stride(0), b.stride(0), out.stride(0), a_scale.stride(0),
-            b_scale.stride(0), a.data_ptr(), b.data_ptr(), a_scale.data_ptr(), b_scale.data_ptr(), out.data_ptr(),
-            status.data_ptr(), _stream(stream), launch_hint & _UINT32, 0))
-    if st != DVP_OK:
-        raise DvpError(st, "dvp_gemm_fp8")
-    return out, status
+    lib = load_library()
+    res = _host.gemm_fp8(lib.at["dvp_gemm_fp8"], a, a_scale, b, b_scale, out_dtype, out, _raw(stream), launch_hint & _UINT32)
+    if type(res) is int:
+        raise DvpError(res, "dvp_gemm_fp8")
+    return res
 
 
 def dvp_sample(logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.0, top_k=0, top_p=1.0, rho=0.0,
@@ -970,37 +875,14 @@ def dvp_sample(logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.0, 
     Returns a namespace with ``ids`` [T] (-1 for a row that has no token to draw or is not finite), ``logp`` = ln pi(a) at the
     temperature, ``logp_mp`` = ln of the same renormalised over what is kept (with ``rho`` alone the ``infer.logp_mp`` of
     ``dvp_forward``) and ``count``, the number of tokens kept."""
-    packed = load_library().packed
-    _check_matrix("logits", logits)
-    T, V = logits.shape
-    if logits.dtype not in _DTYPES:
-        raise TypeError("logits must be float32, bfloat16 or float16")
+    lib = load_library()
     if id_dtype not in (torch.int64, torch.int32):
         raise TypeError("id_dtype must be int64 or int32")
-    _check_vector("uniform", uniform, T, (torch.float32,))
-    values, rows = [], []
-    for name, v, dtype, none in (("temperature", temperature, torch.float32, 1.0), ("top_k", top_k, torch.int32, 0),
-                                 ("top_p", top_p, torch.float32, 1.0), ("rho", rho, torch.float32, 0.0)):
-        if isinstance(v, torch.Tensor):
-            _check_vector(name, v, T, (dtype,))
-            _check_same_device(logits, **{name: v})
-            values.append(none)
-            rows.append(v.data_ptr() if T else 1)
-        else:
-            values.append(v)
-            rows.append(0)
-    _check_same_device(logits, uniform=uniform)
-    f, at, step = _host.outputs(logits, T, 2, 1)
-    ids = logits.new_empty(T, dtype=id_dtype)
-    with _on_device_of(logits):
-        st = packed["dvp_sample"](_SAMPLE_PACK.pack(
-            _SAMPLE_PACK.size, _DTYPES[logits.dtype], DVP_ID_I64 if id_dtype == torch.int64 else DVP_ID_I32,
-            launch_hint & _UINT32, T, V, logits.stride(0), logits.data_ptr(), uniform.data_ptr(), float(values[0]),
-            float(values[2]), float(values[3]), int(values[1]), *rows, ids.data_ptr(), at, at + step, at + 2 * step,
-            _stream(stream)))
-    if st != DVP_OK:
-        raise DvpError(st, "dvp_sample")
-    return SimpleNamespace(ids=ids, logp=f[0], logp_mp=f[1], count=f[2])
+    res = _host.sample(lib.at["dvp_sample"], logits, uniform, temperature, top_k, top_p, rho, id_dtype == torch.int32, _raw(stream),
+                       launch_hint & _UINT32)
+    if type(res) is int:
+        raise DvpError(res, "dvp_sample")
+    return res
 
 
 def dvp_rollout_head(x: torch.Tensor, norm_weight: torch.Tensor, w_vocab: torch.Tensor, w_scale: torch.Tensor,

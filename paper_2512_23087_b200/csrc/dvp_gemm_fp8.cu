@@ -115,14 +115,20 @@ __device__ __forceinline__ void store16(TC *c, const uint64_t *acc, int n, bool 
 
 // ---- many tokens ---------------------------------------------------------------------------------------------------------
 // Block 2 i + r of pair i keeps 128 rows of A, 128 of the 256 rows of B and the 128 x 256 sums of its own rows.  Warp 0: TMA,
-// warp 1: MMA (of the leader, for both), warps 2 to 9: the epilogue, a quarter of the rows and half of the columns each, so that a
+// warp 1: MMA (of the leader, for both), warps 4 to 11: the epilogue, a quarter of the rows and half of the columns each, so that a
 // thread holds 128 sums.  A slice's MMAs take some 512 clocks of an SM, its 64 packed multiply-adds a thread, two warps a
-// scheduler, 256, beside which the tensor memory is read.
-constexpr int kThreads8 = 320;
+// scheduler, 256, and tensor memory is read beside them: the next 32 columns while 32 are added.  For that the epilogue's warps
+// take over registers of the others: 168 a thread at launch, 56 and 224 then, which is the same sum.
+constexpr int kThreads8 = 384;
 constexpr int kEpilogueWarps = 8;
+constexpr int kRegsLaunch = 168, kRegsFew = 56, kRegsMany = 224;
+static_assert(kRegsFew + 2 * kRegsMany <= 3 * kRegsLaunch, "setmaxnreg waits for registers that the block does not have");
 constexpr uint32_t kBytesA8 = 128 * kBlock, kStageBytes8 = 2 * kBytesA8;
 constexpr int kStages8 = 6;
-constexpr size_t kSmemBytes8 = 1024 + (size_t)kStages8 * kStageBytes8 + 256;
+constexpr int kTurnLd = 33;  // 32 x 32 values of a warp, turned so that lanes store neighbouring columns
+constexpr size_t kTurnBytes = (size_t)kEpilogueWarps * 32 * kTurnLd * 4;
+constexpr size_t kSmemBytes8 = 1024 + (size_t)kStages8 * kStageBytes8 + 256 + kTurnBytes;
+static_assert(kSmemBytes8 <= 227 * 1024, "shared memory of a block");
 
 struct Shared8 {
   uint64_t full[kStages8], empty[kStages8], tmem_full[2], tmem_empty[2];
@@ -175,8 +181,10 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const uint32_t tmem_base = sh->tmem_base;
   volatile int *abort_flag = &sh->abort_flag;
 
-  if (warp == 0) {
-    if (lane == 0) {
+  __syncwarp();
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    if (warp == 0 && lane == 0) {
       uint32_t it = 0;
       for (int tile = pair; tile < n_tiles && !*abort_flag; tile += n_pairs) {
         const int tm = m_fastest ? tile % tiles_m : tile / tiles_n, tn = m_fastest ? tile / tiles_m : tile % tiles_n;
@@ -193,9 +201,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           tma_load_2d_pair(dst + kBytesA8, &map_b, bar, ks * kBlock, tn * 256 + (int)rank * 128);
         }
       }
-    }
-  } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    } else if (warp == 1 && lane == 0 && rank == 0) {
       const uint32_t idesc = instr_desc8(256, 256);
       uint32_t it = 0;
       for (int tile = pair; tile < n_tiles && !*abort_flag; tile += n_pairs) {
@@ -225,7 +231,9 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       }
     }
   } else {
-    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    float *turn = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(sh) + 256) + (warp - 4) * 32 * kTurnLd;
     uint32_t it = 0;
     bool ok = true;
     for (int tile = pair; tile < n_tiles && ok; tile += n_pairs) {
@@ -251,25 +259,57 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         }
         tc_fence_after();
         const uint32_t at = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * 256 + half * 128;
+        uint32_t ra[32], rb[32];
+        tmem_ld32(at, ra);
+        tmem_wait_ld(ra);
+        tmem_ld32(at + 32, rb);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          uint32_t r[16];
-          tmem_ld16_wait(at + 16 * c, r);
-          if (c == 7) {  // all has been read
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(map_to_rank(smem_u32(&sh->tmem_empty[buf]), 0));
-          }
+        for (int j = 0; j < 16; ++j) fma2(acc[0 + j], pack2(ra[2 * j], ra[2 * j + 1]), s2);
+        tmem_wait_ld(rb);
+        tmem_ld32(at + 64, ra);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) fma2(acc[8 * c + j], pack2(r[2 * j], r[2 * j + 1]), s2);
-        }
+        for (int j = 0; j < 16; ++j) fma2(acc[16 + j], pack2(rb[2 * j], rb[2 * j + 1]), s2);
+        tmem_wait_ld(ra);
+        tmem_ld32(at + 96, rb);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) fma2(acc[32 + j], pack2(ra[2 * j], ra[2 * j + 1]), s2);
+        tmem_wait_ld(rb);
+        tc_fence_before();  // all has been read
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(map_to_rank(smem_u32(&sh->tmem_empty[buf]), 0));
+#pragma unroll
+        for (int j = 0; j < 16; ++j) fma2(acc[48 + j], pack2(rb[2 * j], rb[2 * j + 1]), s2);
         scale = sa_next * sb_next;
       }
-      if (ok && row < p.M) {
+      if (ok && p.vec) {
         TC *c = static_cast<TC *>(p.C) + (long long)row * p.ldc + col0;
+        if (row < p.M) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (col0 + 16 * j < p.N) store16(c + 16 * j, acc + 8 * j, p.N - (col0 + 16 * j), p.vec != 0);
+          for (int j = 0; j < 8; ++j)
+            if (col0 + 16 * j < p.N) store16(c + 16 * j, acc + 8 * j, p.N - (col0 + 16 * j), true);
+        }
+      } else if (ok) {
+        // Rows that lie anyhow: a thread's own row value by value touched a sector for each (163 x 45,277 float32, K = 416: 72 us a call)
+        const int row0 = row - lane;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (col0 + 32 * q >= p.N) break;
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float lo, hi;
+            unpack2(acc[16 * q + j], lo, hi);
+            turn[lane * kTurnLd + 2 * j] = lo;
+            turn[lane * kTurnLd + 2 * j + 1] = hi;
+          }
+          __syncwarp();
+          const int col = col0 + 32 * q + lane, rows = min(32, p.M - row0);
+          TC *c = static_cast<TC *>(p.C) + (long long)row0 * p.ldc + col;
+          if (col < p.N) {
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r) c[(long long)r * p.ldc] = Storage<TC>::narrow(turn[r * kTurnLd + lane]);
+          }
+        }
       }
     }
   }
@@ -295,7 +335,8 @@ constexpr int kThreadsFew = 192;  // warp 0: TMA, warp 1: MMA, warps 2 to 5: epi
 
 template <int NT>
 struct Few {
-  static constexpr uint32_t kBytesB = 128 * kBlock, kBytesX = NT * kBlock, kStage = kBytesB + kBytesX;
+  // two slices a stage: a row of B is asked for in 256 neighbouring bytes, not 128 here and the next some time later
+  static constexpr uint32_t kBytesB = 128 * kBlock, kBytesX = NT * kBlock, kSlice = kBytesB + kBytesX, kStage = 2 * kSlice;
   static constexpr int kStages = (int)(200 * 1024 / kStage), kAccs = NT <= 64 ? 8 : 4;
   static constexpr uint32_t kCols = NT * kAccs < 512 ? (NT * kAccs) : 512;
   struct Shared {
@@ -347,44 +388,49 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     if (lane == 0) {
       uint32_t it = 0;
       for (int tile = blockIdx.x; tile < tiles && !*abort_flag; tile += gridDim.x)
-        for (int ks = 0; ks < slices; ++ks, ++it) {
+        for (int ks = 0; ks < slices; ks += 2, ++it) {
           const uint32_t s = it % F::kStages, round = it / F::kStages;
           if (round > 0 && !mbar_wait(smem_u32(&sh->empty[s]), (round - 1) & 1, abort_flag)) {
             give_up(abort_flag, p.status, kErrProducerWait);
             break;
           }
           const uint32_t bar = smem_u32(&sh->full[s]), dst = base + s * F::kStage;
-          mbar_expect_tx(bar, (uint32_t)(p.tile_rows + NT) * kBlock);
-          tma_load_2d(dst, &map_b, bar, ks * kBlock, tile * p.tile_rows);
-          tma_load_2d(dst + F::kBytesB, &map_x, bar, ks * kBlock, 0);
+          const int n = min(2, slices - ks);
+          mbar_expect_tx(bar, (uint32_t)(p.tile_rows + NT) * kBlock * n);
+          for (int h = 0; h < n; ++h) tma_load_2d(dst + h * F::kSlice, &map_b, bar, (ks + h) * kBlock, tile * p.tile_rows);
+          for (int h = 0; h < n; ++h) tma_load_2d(dst + h * F::kSlice + F::kBytesB, &map_x, bar, (ks + h) * kBlock, 0);
         }
     }
   } else if (warp == 1) {
     if (lane == 0) {
       const uint32_t idesc = instr_desc8(128, NT);
-      uint32_t it = 0;
+      uint32_t it = 0, sums = 0;
       bool ok = true;
       for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x)
-        for (int ks = 0; ks < slices; ++ks, ++it) {
-          const uint32_t s = it % F::kStages, round = it / F::kStages, buf = it % F::kAccs, use = it / F::kAccs;
-          if (use > 0 && !mbar_wait(smem_u32(&sh->tmem_empty[buf]), (use - 1) & 1, abort_flag)) {
-            give_up(abort_flag, p.status, kErrMmaWaitTmem);
-            ok = false;
-            break;
-          }
+        for (int ks = 0; ks < slices && ok; ks += 2, ++it) {
+          const uint32_t s = it % F::kStages, round = it / F::kStages;
           if (!mbar_wait(smem_u32(&sh->full[s]), round & 1, abort_flag)) {
             give_up(abort_flag, p.status, kErrMmaWaitFull);
             ok = false;
             break;
           }
-          tc_fence_after();
-          const uint32_t b_addr = base + s * F::kStage;
-          const uint64_t bdesc = smem_desc_sw128(b_addr), xdesc = smem_desc_sw128(b_addr + F::kBytesB);
+          const int n = min(2, slices - ks);
+          for (int h = 0; h < n; ++h, ++sums) {  // every slice has an accumulator of its own
+            const uint32_t buf = sums % F::kAccs, use = sums / F::kAccs;
+            if (use > 0 && !mbar_wait(smem_u32(&sh->tmem_empty[buf]), (use - 1) & 1, abort_flag)) {
+              give_up(abort_flag, p.status, kErrMmaWaitTmem);
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t b_addr = base + s * F::kStage + h * F::kSlice;
+            const uint64_t bdesc = smem_desc_sw128(b_addr), xdesc = smem_desc_sw128(b_addr + F::kBytesB);
 #pragma unroll
-          for (int k = 0; k < kBlock / kUmmaK8; ++k)
-            umma8(tmem_base + buf * NT, bdesc + k * (kUmmaK8 >> 4), xdesc + k * (kUmmaK8 >> 4), idesc, k > 0 ? 1u : 0u);
-          umma_commit(smem_u32(&sh->empty[s]));
-          umma_commit(smem_u32(&sh->tmem_full[buf]));
+            for (int k = 0; k < kBlock / kUmmaK8; ++k)
+              umma8(tmem_base + buf * NT, bdesc + k * (kUmmaK8 >> 4), xdesc + k * (kUmmaK8 >> 4), idesc, k > 0 ? 1u : 0u);
+            umma_commit(smem_u32(&sh->tmem_full[buf]));
+          }
+          if (ok) umma_commit(smem_u32(&sh->empty[s]));
         }
     }
   } else {
@@ -554,6 +600,12 @@ cudaError_t launch_pair(const dvp_gemm_fp8_args *a, const Params8 &p, int sms, c
   if (!make_map8(&map_a, a->a, a->M, a->K, a->lda, 128) || !make_map8(&map_b, a->b, a->N, a->K, a->ldb, 128))
     return cudaErrorInvalidValue;
   auto kernel = gemm_fp8_pair_kernel<TC>;
+  // the split of the registers is good for a block that has as many as it was compiled for
+  static const bool as_compiled = [&] {
+    cudaFuncAttributes f;
+    return cudaFuncGetAttributes(&f, kernel) == cudaSuccess && f.numRegs >= kRegsLaunch;
+  }();
+  if (!as_compiled) return cudaErrorLaunchOutOfResources;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes8);
   if (e != cudaSuccess) return e;
   const long long tiles = ((a->M + 255) / 256) * ((a->N + 255) / 256);

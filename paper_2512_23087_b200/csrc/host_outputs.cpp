@@ -1,4 +1,5 @@
-// Python helper: the per-token outputs of a call as views of one allocation, and the marshalling of dvp_forward.
+// Python helper: the per-token outputs of a call as views of one allocation, and the marshalling of dvp_forward and of the
+// rollout's calls.
 //
 // A call has up to twenty output vectors.  Sliced from three allocations through Python they took more than half of
 // the 33 us that a call of dvp_forward on a few tokens spends on the host; as tensors laid directly over one
@@ -7,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/Exceptions.h>
@@ -99,7 +101,15 @@ struct Names {
       *grad_train, *weight, *ns;
 } g_names;
 
+struct MoreNames {
+  PyObject *y, *scale, *rstd, *residual, *d_x, *d_weight, *ids;
+} g_more;
+
 bool make_names() {
+  const char *more[] = {"y", "scale", "rstd", "residual", "d_x", "d_weight", "ids"};
+  PyObject **to = &g_more.y;
+  for (const char *t : more)
+    if (!(*to++ = PyUnicode_InternFromString(t))) return false;
   const char *text[] = {"max", "lse", "lse_safe", "logp", "logp_mp", "comp_mp", "log_cov", "count", "mask", "train",
                         "infer", "log_ratio", "flags", "grad_train", "weight"};
   PyObject **at = &g_names.max;
@@ -247,10 +257,284 @@ PyObject *forward(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the rollout's last stage -------------------------------------------------------------------------------------------
+// What binding's functions of these names do beside the library's call.  A decoding step's calls are a few microseconds of
+// the device's each.
+
+bool given(PyObject *o) { return o != Py_None; }
+void *stream_of(PyObject *o, int device) {
+  return given(o) ? PyLong_AsVoidPtr(o) : static_cast<void *>(c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream());
+}
+void same_device(const at::Tensor &like, const at::Tensor &x, const char *name) {
+  if (x.device() != like.device()) refuse(PyExc_ValueError, "%s must live on the device of the others", name);
+}
+// A vector of n elements side by side, of one of two types.
+const at::Tensor &vector(PyObject *o, const char *name, int64_t n, at::ScalarType a, at::ScalarType b, const at::Tensor &like) {
+  const at::Tensor &x = tensor(o, name);
+  if (x.dim() != 1 || x.size(0) != n || (n > 1 && x.stride(0) != 1)) refuse(PyExc_ValueError, "%s must be a contiguous vector of the right length", name);
+  if (x.scalar_type() != a && x.scalar_type() != b) refuse(PyExc_TypeError, "%s has a type that is not taken here", name);
+  same_device(like, x, name);
+  return x;
+}
+const at::Tensor &like_matrix(PyObject *o, const char *name, const at::Tensor &like) {
+  const at::Tensor &x = matrix(o, name);
+  if (x.sizes() != like.sizes() || x.scalar_type() != like.scalar_type()) refuse(PyExc_ValueError, "%s must match in shape and type", name);
+  same_device(like, x, name);
+  return x;
+}
+// The code of one of the three types that matrices have here.
+int32_t code_of(at::ScalarType t, const char *name) {
+  if (t != at::kFloat && t != at::kBFloat16 && t != at::kHalf) refuse(PyExc_TypeError, "%s must be float32, bfloat16 or float16", name);
+  return dtype_code(t);
+}
+int32_t out_code(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? DVP_E4M3 : code_of(t, "out_dtype"); }
+at::ScalarType type_of(PyObject *o) {
+  if (!THPDtype_Check(o)) refuse(PyExc_TypeError, "%s must be a torch.dtype", "out_dtype");
+  return reinterpret_cast<THPDtype *>(o)->scalar_type;
+}
+at::Tensor make(const at::Tensor &like, at::IntArrayRef sizes, at::ScalarType type) {
+  return at::empty(sizes, like.options().dtype(type).requires_grad(false));
+}
+PyObject *finish(int status, THPObjectPtr &result) { return status == DVP_OK ? result.release() : PyLong_FromLong(status); }
+
+// rms_norm(entry, x, weight, residual, eps, out_dtype, residual_out, stream)
+PyObject *rms_norm(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  if (n_args != 8) {
+    PyErr_SetString(PyExc_TypeError, "rms_norm takes 8 arguments");
+    return nullptr;
+  }
+  HANDLE_TH_ERRORS
+  const auto entry = reinterpret_cast<int (*)(const dvp_rms_norm_args *)>(PyLong_AsVoidPtr(args[0]));
+  const at::Tensor &x = matrix(args[1], "x");
+  const c10::cuda::CUDAGuard guard(x.device());
+  const int64_t T = x.size(0), H = x.size(1);
+  dvp_rms_norm_args a = {};
+  a.struct_size = sizeof(a);
+  a.x_dtype = code_of(x.scalar_type(), "x");
+  a.T = T, a.H = H;
+  a.ld_x = x.stride(0), a.x = x.data_ptr();
+  const at::Tensor &w = vector(args[2], "weight", H, x.scalar_type(), at::kFloat, x);
+  a.weight_dtype = dtype_code(w.scalar_type()), a.weight = w.data_ptr();
+  a.eps = PyFloat_AsDouble(args[4]);
+  if (PyErr_Occurred()) throw python_error();
+  const at::ScalarType out = given(args[5]) ? type_of(args[5]) : x.scalar_type();
+  a.out_dtype = out_code(out);
+  a.stream = stream_of(args[7], x.get_device());
+  THPObjectPtr d(PyDict_New());
+  if (!d) throw python_error();
+  at::Tensor h;
+  if (given(args[3])) {
+    const at::Tensor &r = like_matrix(args[3], "residual", x);
+    a.residual = r.data_ptr(), a.ld_residual = r.stride(0);
+  }
+  if (given(args[6]))
+    h = like_matrix(args[6], "residual_out", x);
+  else if (given(args[3]))
+    h = make(x, {T, H}, x.scalar_type());
+  if (h.defined()) a.residual_out = h.data_ptr(), a.ld_residual_out = h.stride(0);
+  const bool fp8 = a.out_dtype == DVP_E4M3;
+  // 8-bit rows start on 16-byte boundaries, where the tensor cores' loads want them
+  at::Tensor y = fp8 ? make(x, {T, (H + 15) / 16 * 16}, out) : make(x, {T, H}, out);
+  a.out = y.data_ptr(), a.ld_out = y.stride(0);
+  if (fp8 && y.size(1) != H) y = y.narrow(1, 0, H);
+  // rstd and the scales over one storage
+  const int64_t blocks = (H + 127) / 128, rows = (T + 3) / 4 * 16;
+  const at::Tensor buf = make(x, {rows + (fp8 ? T * blocks * 4 : 0)}, at::kByte);
+  a.rstd = static_cast<float *>(buf.data_ptr());
+  const at::Tensor rstd = row_view(buf.storage(), buf.key_set(), at::kFloat, 0, rows, T);
+  if (fp8) {
+    a.scale = reinterpret_cast<float *>(static_cast<char *>(buf.data_ptr()) + rows);
+    a.ld_scale = blocks;
+    put(d.get(), g_more.scale, THPVariable_Wrap(row_view(buf.storage(), buf.key_set(), at::kFloat, 1, rows, T * blocks).view({T, blocks})));
+  } else {
+    put(d.get(), g_more.scale, none());
+  }
+  put(d.get(), g_more.y, THPVariable_Wrap(y));
+  put(d.get(), g_more.rstd, THPVariable_Wrap(rstd));
+  put(d.get(), g_more.residual, h.defined() ? THPVariable_Wrap(h) : none());
+  THPObjectPtr result(namespace_of(d.get()));
+  int status;
+  Py_BEGIN_ALLOW_THREADS status = entry(&a);
+  Py_END_ALLOW_THREADS return finish(status, result);
+  END_HANDLE_TH_ERRORS
+}
+
+// rms_norm_backward(entry, workspace_bytes, dy, h, weight, rstd, d_residual, d_weight, accumulate, workspace, stream)
+PyObject *rms_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  if (n_args != 11) {
+    PyErr_SetString(PyExc_TypeError, "rms_norm_backward takes 11 arguments");
+    return nullptr;
+  }
+  HANDLE_TH_ERRORS
+  const auto entry = reinterpret_cast<int (*)(const dvp_rms_norm_backward_args *)>(PyLong_AsVoidPtr(args[0]));
+  const auto bytes = reinterpret_cast<size_t (*)(int, const void *)>(PyLong_AsVoidPtr(args[1]));
+  const at::Tensor &dy = matrix(args[2], "dy"), &h = matrix(args[3], "h");
+  if (dy.sizes() != h.sizes()) refuse(PyExc_ValueError, "%s must match h in shape", "dy");
+  same_device(h, dy, "dy");
+  const c10::cuda::CUDAGuard guard(h.device());
+  const int64_t T = h.size(0), H = h.size(1);
+  dvp_rms_norm_backward_args a = {};
+  a.struct_size = sizeof(a);
+  a.h_dtype = code_of(h.scalar_type(), "h"), a.dy_dtype = code_of(dy.scalar_type(), "dy");
+  a.T = T, a.H = H;
+  a.dy = dy.data_ptr(), a.ld_dy = dy.stride(0);
+  a.h = h.data_ptr(), a.ld_h = h.stride(0);
+  const at::Tensor &w = vector(args[4], "weight", H, h.scalar_type(), at::kFloat, h);
+  a.weight_dtype = dtype_code(w.scalar_type()), a.weight = w.data_ptr();
+  a.rstd = static_cast<const float *>(vector(args[5], "rstd", T, at::kFloat, at::kFloat, h).data_ptr());
+  if (given(args[6])) {
+    const at::Tensor &r = like_matrix(args[6], "d_residual", h);
+    a.d_residual = r.data_ptr(), a.ld_d_residual = r.stride(0);
+  }
+  a.accumulate_dw = PyObject_IsTrue(args[8]);
+  if (a.accumulate_dw && !given(args[7])) refuse(PyExc_ValueError, "%s needs d_weight", "accumulate_dw");
+  const at::Tensor d_weight = given(args[7]) ? vector(args[7], "d_weight", H, at::kFloat, at::kFloat, h) : make(h, {H}, at::kFloat);
+  a.d_weight = static_cast<float *>(d_weight.data_ptr());
+  const at::Tensor d_x = make(h, {T, H}, h.scalar_type());
+  a.d_x = d_x.data_ptr(), a.ld_d_x = d_x.stride(0);
+  at::Tensor workspace;
+  if (given(args[9])) {
+    workspace = tensor(args[9], "workspace");
+    same_device(h, workspace, "workspace");
+  } else {
+    workspace = make(h, {static_cast<int64_t>(std::max<size_t>(bytes(DVP_ENTRY_RMS_NORM_BACKWARD, &a), 256))}, at::kByte);
+  }
+  a.workspace = workspace.data_ptr();
+  a.workspace_bytes = static_cast<size_t>(workspace.numel() * workspace.element_size());
+  a.stream = stream_of(args[10], h.get_device());
+  THPObjectPtr d(PyDict_New());
+  if (!d) throw python_error();
+  put(d.get(), g_more.d_x, THPVariable_Wrap(d_x));
+  put(d.get(), g_more.d_weight, THPVariable_Wrap(d_weight));
+  THPObjectPtr result(namespace_of(d.get()));
+  int status;
+  Py_BEGIN_ALLOW_THREADS status = entry(&a);
+  Py_END_ALLOW_THREADS return finish(status, result);
+  END_HANDLE_TH_ERRORS
+}
+
+// gemm_fp8(entry, a, a_scale, b, b_scale, out_dtype, out, stream, hint) -> (out, status tensor)
+PyObject *gemm_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  if (n_args != 9) {
+    PyErr_SetString(PyExc_TypeError, "gemm_fp8 takes 9 arguments");
+    return nullptr;
+  }
+  HANDLE_TH_ERRORS
+  const auto entry = reinterpret_cast<int (*)(const dvp_gemm_fp8_args *)>(PyLong_AsVoidPtr(args[0]));
+  const char *names[] = {"a", "a_scale", "b", "b_scale"};
+  const at::Tensor *in[4];
+  for (int i = 0; i < 4; ++i) {
+    in[i] = &matrix(args[1 + i], names[i]);
+    if (in[i]->scalar_type() != (i % 2 ? at::kFloat : at::kFloat8_e4m3fn))
+      refuse(PyExc_TypeError, i % 2 ? "%s must be float32" : "%s must be float8_e4m3fn", names[i]);
+    same_device(*in[0], *in[i], names[i]);
+  }
+  const at::Tensor &x = *in[0], &b = *in[2];
+  const c10::cuda::CUDAGuard guard(x.device());
+  const int64_t M = x.size(0), K = x.size(1), N = b.size(0), blocks = (K + 127) / 128;
+  if (b.size(1) != K) refuse(PyExc_ValueError, "%s and b must have the same number of columns", "a");
+  if (in[1]->size(0) != M || in[1]->size(1) != blocks || in[3]->size(0) != (N + 127) / 128 || in[3]->size(1) != blocks)
+    refuse(PyExc_ValueError, "%s must be [M, ceil(K / 128)] and b_scale [ceil(N / 128), ceil(K / 128)]", "a_scale");
+  at::Tensor out;
+  if (given(args[6])) {
+    out = matrix(args[6], "out");
+    if (out.size(0) != M || out.size(1) != N) refuse(PyExc_ValueError, "%s must be [M, N]", "out");
+    same_device(x, out, "out");
+  }
+  const at::ScalarType type = given(args[6]) ? out.scalar_type() : type_of(args[5]);
+  const int32_t code = code_of(type, "out");
+  if (!out.defined()) out = make(x, {M, N}, type);
+  const at::Tensor status = M && N ? make(x, {1}, at::kInt) : at::zeros({1}, x.options().dtype(at::kInt).requires_grad(false));
+  dvp_gemm_fp8_args a = {};
+  a.struct_size = sizeof(a);
+  a.c_dtype = code;
+  a.M = M, a.N = N, a.K = K;
+  a.lda = x.stride(0), a.ldb = b.stride(0), a.ldc = out.stride(0);
+  a.ld_a_scale = in[1]->stride(0), a.ld_b_scale = in[3]->stride(0);
+  a.a = x.data_ptr(), a.b = b.data_ptr();
+  a.a_scale = static_cast<const float *>(in[1]->data_ptr()), a.b_scale = static_cast<const float *>(in[3]->data_ptr());
+  a.c = out.data_ptr();
+  a.status = static_cast<int32_t *>(status.data_ptr());
+  a.stream = stream_of(args[7], x.get_device());
+  a.launch_hint = static_cast<uint32_t>(PyLong_AsUnsignedLong(args[8]));
+  if (PyErr_Occurred()) throw python_error();
+  THPObjectPtr result(PyTuple_New(2));
+  if (!result) throw python_error();
+  PyTuple_SET_ITEM(result.get(), 0, THPVariable_Wrap(out));
+  PyTuple_SET_ITEM(result.get(), 1, THPVariable_Wrap(status));
+  int st;
+  Py_BEGIN_ALLOW_THREADS st = entry(&a);
+  Py_END_ALLOW_THREADS return finish(st, result);
+  END_HANDLE_TH_ERRORS
+}
+
+// sample(entry, logits, uniform, temperature, top_k, top_p, rho, id32, stream, hint)
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  if (n_args != 10) {
+    PyErr_SetString(PyExc_TypeError, "sample takes 10 arguments");
+    return nullptr;
+  }
+  HANDLE_TH_ERRORS
+  const auto entry = reinterpret_cast<int (*)(const dvp_sample_args *)>(PyLong_AsVoidPtr(args[0]));
+  const at::Tensor &z = matrix(args[1], "logits");
+  const c10::cuda::CUDAGuard guard(z.device());
+  const int64_t T = z.size(0);
+  dvp_sample_args a = {};
+  a.struct_size = sizeof(a);
+  a.logits_dtype = code_of(z.scalar_type(), "logits");
+  a.T = T, a.V = z.size(1), a.ld = z.stride(0);
+  a.logits = z.data_ptr();
+  a.uniform = static_cast<const float *>(vector(args[2], "uniform", T, at::kFloat, at::kFloat, z).data_ptr());
+  // a number for all rows, or one a row; of no rows, no address is looked at, but whose it is
+  const auto setting = [&](PyObject *o, const char *name, at::ScalarType type, const void **rows) {
+    if (!THPVariable_Check(o)) return false;
+    *rows = vector(o, name, T, type, type, z).data_ptr();
+    if (!*rows) *rows = a.logits ? a.logits : &a;
+    return true;
+  };
+  const void *rows = nullptr;
+  a.temperature = a.top_p = 1.0;
+  if (setting(args[3], "temperature", at::kFloat, &rows)) a.temperature_rows = static_cast<const float *>(rows);
+  else a.temperature = PyFloat_AsDouble(args[3]);
+  if (setting(args[4], "top_k", at::kInt, &rows)) a.top_k_rows = static_cast<const int32_t *>(rows);
+  else a.top_k = PyLong_AsLongLong(args[4]);
+  if (setting(args[5], "top_p", at::kFloat, &rows)) a.top_p_rows = static_cast<const float *>(rows);
+  else a.top_p = PyFloat_AsDouble(args[5]);
+  if (setting(args[6], "rho", at::kFloat, &rows)) a.rho_rows = static_cast<const float *>(rows);
+  else a.rho = PyFloat_AsDouble(args[6]);
+  const bool id32 = PyObject_IsTrue(args[7]);
+  a.id_dtype = id32 ? DVP_ID_I32 : DVP_ID_I64;
+  a.stream = stream_of(args[8], z.get_device());
+  a.launch_hint = static_cast<uint32_t>(PyLong_AsUnsignedLong(args[9]));
+  if (PyErr_Occurred()) throw python_error();
+  // rows 0 to 3 of the storage: three vectors of 4 bytes a token; behind them the ids
+  Vectors v(z, T, 5);
+  THPObjectPtr d(PyDict_New());
+  if (!d) throw python_error();
+  put(d.get(), g_names.logp, v.make(0, at::kFloat, &a.logp));
+  put(d.get(), g_names.logp_mp, v.make(1, at::kFloat, &a.logp_mp));
+  put(d.get(), g_names.count, v.make(2, at::kInt, &a.count));
+  a.ids = v.base + 3 * v.stride;
+  put(d.get(), g_more.ids, THPVariable_Wrap(row_view(v.buf.storage(), v.keys, id32 ? at::kInt : at::kLong, 3, v.stride, T)));
+  THPObjectPtr result(namespace_of(d.get()));
+  int status;
+  Py_BEGIN_ALLOW_THREADS status = entry(&a);
+  Py_END_ALLOW_THREADS return finish(status, result);
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {{"outputs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(outputs)), METH_FASTCALL,
                           "outputs(like, T, floats, counts) -> (tensors, address, stride)"},
                          {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(forward)), METH_FASTCALL,
                           "dvp_forward's arguments in, its result or the library's status out"},
+                         {"rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm)), METH_FASTCALL,
+                          "dvp_rms_norm's arguments in, its result or the library's status out"},
+                         {"rms_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm_backward)),
+                          METH_FASTCALL, "dvp_rms_norm_backward's arguments in, its result or the library's status out"},
+                         {"gemm_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gemm_fp8)), METH_FASTCALL,
+                          "dvp_gemm_fp8's arguments in, its result or the library's status out"},
+                         {"sample", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(sample)), METH_FASTCALL,
+                          "dvp_sample's arguments in, its result or the library's status out"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
