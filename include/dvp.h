@@ -623,7 +623,7 @@ int dvp_quantize_fp8(const dvp_quantize_fp8_args *args);
  *   b        device [N, ldb] e4m3 (LM-head rows), b_scale device [ceil(N / 128), ld_b_scale] float32
  *   c        device [M, ldc] of c_dtype (DVP_F32, DVP_BF16, DVP_F16), any stride and alignment to its element
  *   status   device int32: 0 after a run in which every kernel finished, non-zero if one gave up waiting (C is then invalid)
- *   launch_hint  0 = library default; 1: the kernel of 256 x 256 tiles; 2: the one for few tokens, M <= 128.  Tuning only:
+ *   launch_hint  0 = library default; 1: the kernel of 256 x 256 tiles; 2: the one for few tokens, M <= 64.  Tuning only:
  *            results differ in the order of the sums alone
  * a and b on 16-byte boundaries, lda and ldb multiples of 16 (DVP_ERR_UNSUPPORTED otherwise); K itself may be any.  Needs no
  * workspace.  M = 0 or N = 0 is a valid no-op.  Errors: DVP_ERR_INVALID_ARG (null pointers, negative sizes, K < 1, short

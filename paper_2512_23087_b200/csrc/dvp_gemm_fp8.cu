@@ -7,7 +7,7 @@
 // multiplied.  That also keeps every sum in the tensor core, which cuts off what does not fit its accumulator, to 128 terms.
 //
 //   many tokens   pairs of blocks on 256 x 256 tiles, as the 16-bit contraction has them; bound by the tensor cores
-//   few tokens    (M <= 128) operands swapped: 128 rows of B are the M of the instruction, the tokens its N; one block streams
+//   few tokens    (M <= 64) operands swapped: 128 rows of B are the M of the instruction, the tokens its N; one block streams
 //                 its rows of B through a deep ring of TMA loads; bound by HBM
 #include <cmath>
 
@@ -70,25 +70,9 @@ __device__ __forceinline__ void tmem_ld16_wait(uint32_t taddr, uint32_t (&r)[16]
                : "memory");
 }
 
-// Two float32 in a 64-bit register: one instruction multiplies and adds both.
-__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
-  uint64_t v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
-  return v;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float &lo, float &hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t x, uint64_t s) {
-  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(x), "l"(s));
-}
-
 // Sixteen neighbouring values of a row of C, the first `n` of which exist.
 template <typename TC>
-__device__ __forceinline__ void store16(TC *c, const uint64_t *acc, int n, bool vec) {
-  float v[16];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) unpack2(acc[j], v[2 * j], v[2 * j + 1]);
+__device__ __forceinline__ void store16(TC *c, const float *v, int n, bool vec) {
   if (vec && n >= 16) {
     uint32_t w[8];
     if constexpr (sizeof(TC) == 4) {
@@ -241,16 +225,15 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       const int row = tm * 256 + (int)rank * 128 + quarter * 32 + lane, col0 = tn * 256 + half * 128;
       const float *sa = p.sa + (long long)(row < p.M ? row : 0) * p.ld_sa;
       const float *sb = p.sb + (long long)(col0 < p.N ? col0 / kBlock : 0) * p.ld_sb;
-      uint64_t acc[64];
+      float acc[128];
 #pragma unroll
-      for (int j = 0; j < 64; ++j) acc[j] = 0;
+      for (int j = 0; j < 128; ++j) acc[j] = 0.f;
       float scale = __ldg(sa) * __ldg(sb);
       for (int ks = 0; ks < slices; ++ks, ++it) {
         const uint32_t buf = it & 1, use = it >> 1;
         // the next slice's scales are fetched while this one's sums are waited for
         const int next = ks + 1 < slices ? ks + 1 : ks;
         const float sa_next = __ldg(sa + next), sb_next = __ldg(sb + next);
-        const uint64_t s2 = pack2(__float_as_uint(scale), __float_as_uint(scale));
         // the whole warp goes on or none of it
         if (!__all_sync(0xffffffffu, !*abort_flag && mbar_wait(smem_u32(&sh->tmem_full[buf]), use & 1, abort_flag))) {
           give_up(abort_flag, p.status, kErrEpilogueWait);
@@ -264,21 +247,21 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         tmem_wait_ld(ra);
         tmem_ld32(at + 32, rb);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) fma2(acc[0 + j], pack2(ra[2 * j], ra[2 * j + 1]), s2);
+        for (int j = 0; j < 32; ++j) acc[0 + j] = fmaf(__uint_as_float(ra[j]), scale, acc[0 + j]);
         tmem_wait_ld(rb);
         tmem_ld32(at + 64, ra);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) fma2(acc[16 + j], pack2(rb[2 * j], rb[2 * j + 1]), s2);
+        for (int j = 0; j < 32; ++j) acc[32 + j] = fmaf(__uint_as_float(rb[j]), scale, acc[32 + j]);
         tmem_wait_ld(ra);
         tmem_ld32(at + 96, rb);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) fma2(acc[32 + j], pack2(ra[2 * j], ra[2 * j + 1]), s2);
+        for (int j = 0; j < 32; ++j) acc[64 + j] = fmaf(__uint_as_float(ra[j]), scale, acc[64 + j]);
         tmem_wait_ld(rb);
         tc_fence_before();  // all has been read
         __syncwarp();
         if (lane == 0) mbar_arrive_remote(map_to_rank(smem_u32(&sh->tmem_empty[buf]), 0));
 #pragma unroll
-        for (int j = 0; j < 16; ++j) fma2(acc[48 + j], pack2(rb[2 * j], rb[2 * j + 1]), s2);
+        for (int j = 0; j < 32; ++j) acc[96 + j] = fmaf(__uint_as_float(rb[j]), scale, acc[96 + j]);
         scale = sa_next * sb_next;
       }
       if (ok && p.vec) {
@@ -286,7 +269,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         if (row < p.M) {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (col0 + 16 * j < p.N) store16(c + 16 * j, acc + 8 * j, p.N - (col0 + 16 * j), true);
+            if (col0 + 16 * j < p.N) store16(c + 16 * j, acc + 16 * j, p.N - (col0 + 16 * j), true);
         }
       } else if (ok) {
         // Rows that lie anyhow: a thread's own row value by value touched a sector for each (163 x 45,277 float32, K = 416: 72 us a call)
@@ -296,12 +279,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           if (col0 + 32 * q >= p.N) break;
           __syncwarp();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            float lo, hi;
-            unpack2(acc[16 * q + j], lo, hi);
-            turn[lane * kTurnLd + 2 * j] = lo;
-            turn[lane * kTurnLd + 2 * j + 1] = hi;
-          }
+          for (int j = 0; j < 32; ++j) turn[lane * kTurnLd + j] = acc[32 * q + j];
           __syncwarp();
           const int col = col0 + 32 * q + lane, rows = min(32, p.M - row0);
           TC *c = static_cast<TC *>(p.C) + (long long)row0 * p.ldc + col;
@@ -331,25 +309,30 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 // A tile is `tile_rows` <= 128 rows of B, so many that all blocks have the same number of tiles (152 thousand rows in tiles of
 // 128 were 1,187 tiles for 148 blocks, nine for some and eight for most); rows of the instruction behind them compute on
 // what the ring held before, and nobody reads their sums.
-constexpr int kThreadsFew = 192;  // warp 0: TMA, warp 1: MMA, warps 2 to 5: epilogue, a row of B a thread
+// Warp 0: TMA, warp 1: MMA, the others: epilogue, a row of B and up to 32 tokens a thread.
+constexpr int kSlicesPerStage = 4;  // a row of B is asked for in so many times 128 bytes (16 x 4,096 x 151,936: 111 us, with two 117)
 
 template <int NT>
 struct Few {
-  // two slices a stage: a row of B is asked for in 256 neighbouring bytes, not 128 here and the next some time later
-  static constexpr uint32_t kBytesB = 128 * kBlock, kBytesX = NT * kBlock, kSlice = kBytesB + kBytesX, kStage = 2 * kSlice;
-  static constexpr int kStages = (int)(200 * 1024 / kStage), kAccs = NT <= 64 ? 8 : 4;
-  static constexpr uint32_t kCols = NT * kAccs < 512 ? (NT * kAccs) : 512;
+  static constexpr int kParts = NT <= 32 ? 1 : NT / 32, kTokens = NT / kParts;  // the epilogue's parts of the tokens
+  static constexpr int kThreads = 64 + 128 * kParts;
+  static constexpr uint32_t kBytesB = 128 * kBlock, kBytesX = NT * kBlock, kSlice = kBytesB + kBytesX,
+                            kStage = kSlicesPerStage * kSlice;
+  static constexpr int kAccs = 8;
+  static constexpr uint32_t kCols = NT * kAccs;
+  static constexpr int kStages = (int)(220 * 1024 / kStage);
   struct Shared {
     uint64_t full[kStages], empty[kStages], tmem_full[kAccs], tmem_empty[kAccs];
     uint32_t tmem_base;
     int abort_flag;
-    float scale[4][2][NT];  // an epilogue warp's token scales of a slice
+    alignas(16) float scale[4 * kParts][2][kTokens];  // read four at a time; an epilogue warp's token scales of a slice
   };
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + sizeof(Shared);
+  static_assert(kSmem <= 227 * 1024 && kCols <= kTmemCols, "a block's room");
 };
 
 template <typename TC, int NT>
-__global__ void __launch_bounds__(kThreadsFew, 1)
+__global__ void __launch_bounds__(Few<NT>::kThreads, 1)
 gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_b, const Params8 p) {
   using F = Few<NT>;
   extern __shared__ uint8_t smem_raw[];
@@ -366,7 +349,7 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     }
     for (int b = 0; b < F::kAccs; ++b) {
       mbar_init(smem_u32(&sh->tmem_full[b]), 1);
-      mbar_init(smem_u32(&sh->tmem_empty[b]), 4);
+      mbar_init(smem_u32(&sh->tmem_empty[b]), 4 * F::kParts);
     }
     sh->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -388,14 +371,14 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     if (lane == 0) {
       uint32_t it = 0;
       for (int tile = blockIdx.x; tile < tiles && !*abort_flag; tile += gridDim.x)
-        for (int ks = 0; ks < slices; ks += 2, ++it) {
+        for (int ks = 0; ks < slices; ks += kSlicesPerStage, ++it) {
           const uint32_t s = it % F::kStages, round = it / F::kStages;
           if (round > 0 && !mbar_wait(smem_u32(&sh->empty[s]), (round - 1) & 1, abort_flag)) {
             give_up(abort_flag, p.status, kErrProducerWait);
             break;
           }
           const uint32_t bar = smem_u32(&sh->full[s]), dst = base + s * F::kStage;
-          const int n = min(2, slices - ks);
+          const int n = min(kSlicesPerStage, slices - ks);
           mbar_expect_tx(bar, (uint32_t)(p.tile_rows + NT) * kBlock * n);
           for (int h = 0; h < n; ++h) tma_load_2d(dst + h * F::kSlice, &map_b, bar, (ks + h) * kBlock, tile * p.tile_rows);
           for (int h = 0; h < n; ++h) tma_load_2d(dst + h * F::kSlice + F::kBytesB, &map_x, bar, (ks + h) * kBlock, 0);
@@ -407,14 +390,14 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       uint32_t it = 0, sums = 0;
       bool ok = true;
       for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x)
-        for (int ks = 0; ks < slices && ok; ks += 2, ++it) {
+        for (int ks = 0; ks < slices && ok; ks += kSlicesPerStage, ++it) {
           const uint32_t s = it % F::kStages, round = it / F::kStages;
           if (!mbar_wait(smem_u32(&sh->full[s]), round & 1, abort_flag)) {
             give_up(abort_flag, p.status, kErrMmaWaitFull);
             ok = false;
             break;
           }
-          const int n = min(2, slices - ks);
+          const int n = min(kSlicesPerStage, slices - ks);
           for (int h = 0; h < n; ++h, ++sums) {  // every slice has an accumulator of its own
             const uint32_t buf = sums % F::kAccs, use = sums / F::kAccs;
             if (use > 0 && !mbar_wait(smem_u32(&sh->tmem_empty[buf]), (use - 1) & 1, abort_flag)) {
@@ -434,59 +417,56 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         }
     }
   } else {
-    const int quarter = warp & 3;
-    float (*mine)[NT] = sh->scale[quarter];
+    const int quarter = warp & 3, part = (warp - 2) >> 2, first = part * F::kTokens;
+    float (*mine)[F::kTokens] = sh->scale[warp - 2];
     uint32_t it = 0;
     bool ok = true;
     for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
       const int in_tile = quarter * 32 + lane, row = tile * p.tile_rows + in_tile;
       const bool live = in_tile < p.tile_rows && row < p.N;
       const float *sb = p.sb + (long long)(live ? row / kBlock : 0) * p.ld_sb;
-      uint64_t acc[NT / 2];
+      const bool token = lane < F::kTokens && first + lane < p.M;  // whose scales this lane fetches
+      const float *sa = p.sa + (long long)(token ? first + lane : 0) * p.ld_sa;
+      float acc[F::kTokens];
 #pragma unroll
-      for (int j = 0; j < NT / 2; ++j) acc[j] = 0;
+      for (int j = 0; j < F::kTokens; ++j) acc[j] = 0.f;
       for (int ks = 0; ks < slices; ++ks, ++it) {
         const uint32_t buf = it % F::kAccs, use = it / F::kAccs;
         const float s = __ldg(sb + ks);
         // two sets: the slice before may still be read by a lane that is behind
         float *scale = mine[it & 1];
-#pragma unroll
-        for (int j = lane; j < NT; j += 32) scale[j] = j < p.M ? __ldg(p.sa + (long long)j * p.ld_sa + ks) : 0.f;
+        if (lane < F::kTokens) scale[lane] = token ? __ldg(sa + ks) : 0.f;
         if (!__all_sync(0xffffffffu, !*abort_flag && mbar_wait(smem_u32(&sh->tmem_full[buf]), use & 1, abort_flag))) {
           give_up(abort_flag, p.status, kErrEpilogueWait);
           ok = false;
           break;
         }
         tc_fence_after();
-        const uint32_t at = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * NT;
-        const uint64_t s2 = pack2(__float_as_uint(s), __float_as_uint(s));
+        const uint32_t at = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * NT + first;
+        uint32_t r[F::kTokens];
+        if constexpr (F::kTokens == 16) {
+          tmem_ld16_wait(at, r);
+        } else {
+          tmem_ld32(at, r);
+          tmem_wait_ld(r);
+        }
+        tc_fence_before();  // all has been read
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->tmem_empty[buf]));
 #pragma unroll
-        for (int c = 0; c < NT / 16; ++c) {
-          uint32_t r[16];
-          tmem_ld16_wait(at + 16 * c, r);
-          if (c == NT / 16 - 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->tmem_empty[buf]));
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const uint64_t t2 = *reinterpret_cast<const uint64_t *>(scale + 16 * c + 2 * j);
-            uint64_t st;
-            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(st) : "l"(t2), "l"(s2));
-            fma2(acc[8 * c + j], pack2(r[2 * j], r[2 * j + 1]), st);
-          }
+        for (int j = 0; j < F::kTokens; j += 4) {
+          const float4 t = *reinterpret_cast<const float4 *>(scale + j);
+          acc[j] = fmaf(__uint_as_float(r[j]), t.x * s, acc[j]);
+          acc[j + 1] = fmaf(__uint_as_float(r[j + 1]), t.y * s, acc[j + 1]);
+          acc[j + 2] = fmaf(__uint_as_float(r[j + 2]), t.z * s, acc[j + 2]);
+          acc[j + 3] = fmaf(__uint_as_float(r[j + 3]), t.w * s, acc[j + 3]);
         }
       }
       if (ok && live) {
-        TC *c = static_cast<TC *>(p.C) + row;
+        TC *c = static_cast<TC *>(p.C) + (long long)first * p.ldc + row;
 #pragma unroll
-        for (int j = 0; j < NT / 2; ++j) {
-          float lo, hi;
-          unpack2(acc[j], lo, hi);
-          if (2 * j < p.M) c[(long long)(2 * j) * p.ldc] = Storage<TC>::narrow(lo);
-          if (2 * j + 1 < p.M) c[(long long)(2 * j + 1) * p.ldc] = Storage<TC>::narrow(hi);
-        }
+        for (int j = 0; j < F::kTokens; ++j)
+          if (first + j < p.M) c[(long long)j * p.ldc] = Storage<TC>::narrow(acc[j]);
       }
     }
   }
@@ -639,17 +619,16 @@ cudaError_t launch_few(const dvp_gemm_fp8_args *a, Params8 p, int sms, cudaStrea
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Few<NT>::kSmem);
   if (e != cudaSuccess) return e;
   const long long tiles = (a->N + rows - 1) / rows;
-  kernel<<<(unsigned)(tiles < sms ? tiles : sms), kThreadsFew, Few<NT>::kSmem, stream>>>(map_x, map_b, p);
+  kernel<<<(unsigned)(tiles < sms ? tiles : sms), Few<NT>::kThreads, Few<NT>::kSmem, stream>>>(map_x, map_b, p);
   return cudaGetLastError();
 }
 
 template <typename TC>
 cudaError_t launch(const dvp_gemm_fp8_args *a, const Params8 &p, int sms, cudaStream_t stream) {
-  if (a->M > 128 || a->launch_hint == 1) return launch_pair<TC>(a, p, sms, stream);
+  if (a->M > 64 || a->launch_hint == 1) return launch_pair<TC>(a, p, sms, stream);
   if (a->M <= 16) return launch_few<TC, 16>(a, p, sms, stream);
   if (a->M <= 32) return launch_few<TC, 32>(a, p, sms, stream);
-  if (a->M <= 64) return launch_few<TC, 64>(a, p, sms, stream);
-  return launch_few<TC, 128>(a, p, sms, stream);
+  return launch_few<TC, 64>(a, p, sms, stream);
 }
 
 template <typename T>
@@ -674,7 +653,7 @@ int dvp_gemm_fp8(const dvp_gemm_fp8_args *a) {
   if (a->M < 0 || a->N < 0 || a->K < 1 || a->launch_hint > 2) return DVP_ERR_INVALID_ARG;
   if (a->M > kMost || a->N > kMost || a->K > kMost) return DVP_ERR_UNSUPPORTED;
   if (((a->M + 255) / 256) * ((a->N + 255) / 256) > kMost) return DVP_ERR_UNSUPPORTED;  // tiles are counted in 32 bits
-  if (a->launch_hint == 2 && a->M > 128) return DVP_ERR_INVALID_ARG;
+  if (a->launch_hint == 2 && a->M > 64) return DVP_ERR_INVALID_ARG;
   if (a->M == 0 || a->N == 0) return DVP_OK;
   if (!a->a || !a->b || !a->a_scale || !a->b_scale || !a->c || !a->status) return DVP_ERR_INVALID_ARG;
   const int64_t blocks = (a->K + kBlock - 1) / kBlock;

@@ -7,6 +7,7 @@
 // Both are bound by HBM: a row's threads hold it in registers between the sum and the output, so every matrix passes
 // once.  Rows that vectors of eight elements do not fit (width, stride or base) have kernels of their own, which read a row
 // twice, element by element.
+#include <atomic>
 #include <cmath>
 
 #include "dvp_common.cuh"
@@ -31,24 +32,36 @@ struct Params {
   int w_f32;
 };
 
-// Eight neighbouring elements.  Not through the read-only path: an output may take the place of an input, whose elements
-// the same thread has read.
+// Eight neighbouring elements as they lie.  Not through the read-only path: an output may take the place of an input, whose
+// elements the same thread has read.
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
-                 : "l"(p)
-                 : "memory");
-  } else {
-    uint4 u;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
-                 : "l"(p)
-                 : "memory");
-    Storage<T>::unpack(u, v);
+struct Raw {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T *p) {
+    if constexpr (sizeof(T) == 4)
+      asm volatile("ld.global.L1::no_allocate.v8.u32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                   : "l"(p)
+                   : "memory");
+    else
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                   : "l"(p)
+                   : "memory");
   }
-}
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int j = 0; j < (int)(2 * sizeof(T)); ++j) w[j] = 0;
+  }
+  __device__ __forceinline__ void widen(float (&v)[8]) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+    } else {
+      Storage<T>::unpack(make_uint4(w[0], w[1], w[2], w[3]), v);
+    }
+  }
+};
 template <typename T>
 __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
@@ -101,62 +114,81 @@ __device__ __forceinline__ float row_sum(float v, int tpr, float *part) {
 
 // ---- rows in vectors ---------------------------------------------------------------------------------------------------
 
+// A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: the next is on its way while one is summed up and stored, so that loads
+// never pause (16,384 x 4,096 bfloat16 to 8 bits: FWD_NOW us, with one row a block and nothing on its way 139).
 template <typename T, typename TOut, int kPer>
-__global__ void __launch_bounds__(1024, 1) rms_norm_kernel(const Params p, const int tpr) {
-  __shared__ float part[32];
-  const int lane_of_row = threadIdx.x % tpr;
-  const long long t = (long long)blockIdx.x * (blockDim.x / tpr) + threadIdx.x / tpr;
-  const bool live = t < p.T;
-  float h[kPer][kVec], w[kPer][kVec];
-  float sum = 0.f;
+__global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rms_norm_kernel(const Params p, const int tpr) {
+  __shared__ float part[2][32];
+  const int lane_of_row = threadIdx.x % tpr, rpb = blockDim.x / tpr;
+  const long long step = (long long)gridDim.x * rpb;
+  Raw<T> x[kPer], r[kPer];
+  const auto column = [&](int i) { return ((long long)lane_of_row + (long long)i * tpr) * kVec; };
+  const auto fetch = [&](long long t) {
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
-    if (live && c < p.H) {
-      load8(static_cast<const T *>(p.x) + t * p.ld_x + c, h[i]);
-      if (p.r) {
-        float r[kVec];
-        load8(static_cast<const T *>(p.r) + t * p.ld_r + c, r);
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) h[i][j] += r[j];
+    for (int i = 0; i < kPer; ++i) {
+      const long long c = column(i);
+      if (t < p.T && c < p.H) {
+        x[i].load(static_cast<const T *>(p.x) + t * p.ld_x + c);
+        if (p.r) r[i].load(static_cast<const T *>(p.r) + t * p.ld_r + c);
+      } else {
+        x[i].zero();
+        r[i].zero();
       }
-      load_weights8<T>(p.w, p.w_f32, c, w[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) h[i][j] = w[i][j] = 0.f;
     }
-  }
+  };
+  long long t = (long long)blockIdx.x * rpb + threadIdx.x / tpr;
+  fetch(t);
+  int turn = 0;
+  for (long long first = (long long)blockIdx.x * rpb; first < p.T; first += step, t += step, turn ^= 1) {
+    const bool live = t < p.T;
+    float h[kPer][kVec], sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i)
+    for (int i = 0; i < kPer; ++i) {
+      x[i].widen(h[i]);
+      if (p.r) {
+        float v[kVec];
+        r[i].widen(v);
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) sum = fmaf(h[i][j], h[i][j], sum);
-  const float s = 1.f / sqrtf(fmaf(row_sum(sum, tpr, part), p.inv_h, p.eps));
-  if (live && lane_of_row == 0 && p.rstd) p.rstd[t] = s;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
-    const bool here = live && c < p.H;
-    if (p.r_out && here) store8(static_cast<T *>(p.r_out) + t * p.ld_r_out + c, h[i]);
-    float y[kVec];
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) y[j] = h[i][j] * s * w[i][j];
-    if constexpr (sizeof(TOut) == 1) {
-      // sixteen neighbouring lanes hold a block of 128 columns
-      float a = kLeastAmax;
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) a = fmaxf(a, fabsf(y[j]));
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-      const float scale = a / kFp8Max, inv = 1.f / scale;
-      if (here) {
-        if ((threadIdx.x & 15) == 0) p.scale[t * p.ld_scale + c / kBlockCols] = scale;
-        uint2 q;
-        q.x = fp8_pair(y[0] * inv, y[1] * inv) | fp8_pair(y[2] * inv, y[3] * inv) << 16;
-        q.y = fp8_pair(y[4] * inv, y[5] * inv) | fp8_pair(y[6] * inv, y[7] * inv) << 16;
-        st_stream8(static_cast<uint8_t *>(p.out) + t * p.ld_out + c, q);
+        for (int j = 0; j < kVec; ++j) h[i][j] += v[j];
       }
-    } else if (here) {
-      store8(static_cast<TOut *>(p.out) + t * p.ld_out + c, y);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) sum = fmaf(h[i][j], h[i][j], sum);
+    }
+    if (first + step < p.T) fetch(t + step);
+    const float s = 1.f / sqrtf(fmaf(row_sum(sum, tpr, part[turn]), p.inv_h, p.eps));  // two sets: see the backward kernel
+    if (live && lane_of_row == 0 && p.rstd) p.rstd[t] = s;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const long long c = column(i);
+      const bool here = live && c < p.H;
+      if (p.r_out && here) store8(static_cast<T *>(p.r_out) + t * p.ld_r_out + c, h[i]);
+      float w[kVec], y[kVec];
+      if (here) {
+        load_weights8<T>(p.w, p.w_f32, c, w);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) w[j] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) y[j] = h[i][j] * s * w[j];
+      if constexpr (sizeof(TOut) == 1) {
+        // sixteen neighbouring lanes hold a block of 128 columns
+        float a = kLeastAmax;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) a = fmaxf(a, fabsf(y[j]));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+        const float scale = a / kFp8Max, inv = 1.f / scale;
+        if (here) {
+          if ((threadIdx.x & 15) == 0) p.scale[t * p.ld_scale + c / kBlockCols] = scale;
+          uint2 q;
+          q.x = fp8_pair(y[0] * inv, y[1] * inv) | fp8_pair(y[2] * inv, y[3] * inv) << 16;
+          q.y = fp8_pair(y[4] * inv, y[5] * inv) | fp8_pair(y[6] * inv, y[7] * inv) << 16;
+          st_stream8(static_cast<uint8_t *>(p.out) + t * p.ld_out + c, q);
+        }
+      } else if (here) {
+        store8(static_cast<TOut *>(p.out) + t * p.ld_out + c, y);
+      }
     }
   }
 }
@@ -244,7 +276,7 @@ struct BackParams {
 
 // A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: its threads keep their columns, and with them the sums of dw.
 template <typename T, typename TD, int kPer>
-__global__ void __launch_bounds__(512, 1) rms_norm_backward_kernel(const BackParams p, const int tpr) {
+__global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rms_norm_backward_kernel(const BackParams p, const int tpr) {
   __shared__ float part[2][32];
   const int lane_of_row = threadIdx.x % tpr, rpb = blockDim.x / tpr, row_of_block = threadIdx.x / tpr;
   float w[kPer][kVec], dw[kPer][kVec];
@@ -255,33 +287,51 @@ __global__ void __launch_bounds__(512, 1) rms_norm_backward_kernel(const BackPar
     for (int j = 0; j < kVec; ++j) w[i][j] = dw[i][j] = 0.f;
     if (c < p.H) load_weights8<T>(p.w, p.w_f32, c, w[i]);
   }
+  const long long step = (long long)gridDim.x * rpb;
+  Raw<T> h_raw[kPer], r_raw[kPer];
+  Raw<TD> d_raw[kPer];
+  const auto fetch = [&](long long t) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
+      if (t < p.T && c < p.H) {
+        d_raw[i].load(static_cast<const TD *>(p.dy) + t * p.ld_dy + c);
+        h_raw[i].load(static_cast<const T *>(p.h) + t * p.ld_h + c);
+        if (p.dr) r_raw[i].load(static_cast<const T *>(p.dr) + t * p.ld_dr + c);
+      } else {
+        d_raw[i].zero();
+        h_raw[i].zero();
+        r_raw[i].zero();
+      }
+    }
+  };
+  constexpr bool kAhead = kPer < 4;  // four vectors a thread leave no registers for the next row
+  long long t = (long long)blockIdx.x * rpb + row_of_block;
+  if (kAhead) fetch(t);
+  float s_next = t < p.T ? p.rstd[t] : 0.f;
   int turn = 0;
-  for (long long t0 = (long long)blockIdx.x * rpb; t0 < p.T; t0 += (long long)gridDim.x * rpb, turn ^= 1) {
-    const long long t = t0 + row_of_block;
+  for (long long first = (long long)blockIdx.x * rpb; first < p.T; first += step, t += step, turn ^= 1) {
     const bool live = t < p.T;
-    const float s = live ? p.rstd[t] : 0.f;
+    const float s = s_next;
+    if (!kAhead) fetch(t);
     float h[kPer][kVec], d[kPer][kVec], r[kPer][kVec];
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const long long c = ((long long)lane_of_row + (long long)i * tpr) * kVec;
-      if (live && c < p.H) {
-        load8(static_cast<const TD *>(p.dy) + t * p.ld_dy + c, d[i]);
-        load8(static_cast<const T *>(p.h) + t * p.ld_h + c, h[i]);
-        if (p.dr) load8(static_cast<const T *>(p.dr) + t * p.ld_dr + c, r[i]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) d[i][j] = h[i][j] = 0.f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
+      h_raw[i].widen(h[i]);
+      d_raw[i].widen(d[i]);
+      if (p.dr) r_raw[i].widen(r[i]);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
         dw[i][j] = fmaf(d[i][j] * s, h[i][j], dw[i][j]);
         d[i][j] *= w[i][j];
         dot = fmaf(d[i][j], h[i][j], dot);
       }
+    }
+    if (first + step < p.T) {
+      if (kAhead) fetch(t + step);
+      s_next = t + step < p.T ? p.rstd[t + step] : 0.f;
+    }
     dot = row_sum(dot, tpr, part[turn]);  // two sets: one is read while the next row's is written
     const float k = dot * p.inv_h * s * s;
     if (p.dx && live) {
@@ -365,14 +415,28 @@ inline bool weight_vectors(const void *w) { return (uintptr_t)w % 16 == 0; }
 struct Shape {
   int per, tpr, rpb;  // vectors a thread, threads a row, rows a block
 };
-// Two vectors a thread where the row has enough of them, so that a row of 4,096 is eight warps with 32 bytes a thread and
-// matrix in flight.  per = 0: too long for the registers, or no vector at all.
-inline Shape shape_of(long long H, bool backward) {
+// One vector a thread up to 512 threads a row, then more.  per = 0: too long for the registers, or no vector at all.
+inline Shape shape_of(long long H) {
   const long long nv = H / kVec;
-  const int per = nv < 1 ? 0 : nv <= 64 ? 1 : nv <= (backward ? 1024 : 2048) ? 2 : backward && nv <= 2048 ? 4 : 0;
+  const int per = nv < 1 ? 0 : nv <= 512 ? 1 : nv <= 1024 ? 2 : nv <= 2048 ? 4 : 0;
   if (!per) return {0, 0, 0};
   const int tpr = (int)(((nv + per - 1) / per + 31) / 32 * 32);
   return {per, tpr, tpr >= 256 ? 1 : 256 / tpr};
+}
+// Blocks that the chip holds at once: what a kernel's registers allow, asked for once a kernel and number of threads.
+template <typename Kernel>
+int resident(Kernel kernel, std::atomic<int> (&known)[33], int threads, int sms) {
+  int blocks = known[threads / 32].load(std::memory_order_relaxed);
+  if (blocks == 0) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, threads, 0) != cudaSuccess || blocks < 1) blocks = 1;
+    known[threads / 32].store(blocks, std::memory_order_relaxed);
+  }
+  return blocks * sms;
+}
+inline int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) return 148;
+  return sms;
 }
 
 // Calls f with a value of the storage type that `d` names.
@@ -385,40 +449,54 @@ cudaError_t by_type(int d, F f) {
 
 template <typename T, typename TOut>
 cudaError_t launch_forward(const Params &p, bool fast, cudaStream_t stream) {
-  const Shape sh = shape_of(p.H, false);
+  const Shape sh = shape_of(p.H);
   if (fast && sh.per) {
-    const unsigned grid = (unsigned)((p.T + sh.rpb - 1) / sh.rpb), block = (unsigned)(sh.tpr * sh.rpb);
+    const int block = sh.tpr * sh.rpb;
+    const long long want = (p.T + sh.rpb - 1) / sh.rpb;
+    static std::atomic<int> known[5][33];
+    const auto go = [&](auto kernel) {
+      const long long most = resident(kernel, known[sh.per], block, sm_count());
+      kernel<<<(unsigned)(want < most ? want : most), block, 0, stream>>>(p, sh.tpr);
+    };
     if (sh.per == 1)
-      rms_norm_kernel<T, TOut, 1><<<grid, block, 0, stream>>>(p, sh.tpr);
+      go(rms_norm_kernel<T, TOut, 1>);
+    else if (sh.per == 2)
+      go(rms_norm_kernel<T, TOut, 2>);
     else
-      rms_norm_kernel<T, TOut, 2><<<grid, block, 0, stream>>>(p, sh.tpr);
+      go(rms_norm_kernel<T, TOut, 4>);
   } else {
     rms_norm_any_kernel<T, TOut><<<(unsigned)p.T, kAnyThreads, 0, stream>>>(p);
   }
   return cudaGetLastError();
 }
 
-// Blocks of the backward kernel: what the chip holds at once, no more than there are rows.
-inline int backward_blocks(long long T, int rpb) {
-  const long long want = (T + rpb - 1) / rpb, most = kMaxPartials / rpb;
-  return (int)(want < most ? want : most);
+// Blocks of the backward kernel: what the chip holds at once and the workspace has rows for, no more than there are rows.
+inline int backward_blocks(long long T, int rpb, int most_blocks) {
+  const long long want = (T + rpb - 1) / rpb, room = kMaxPartials / rpb;
+  const long long n = want < room ? want : room;
+  return (int)(n < most_blocks ? n : most_blocks);
 }
 
 template <typename T, typename TD>
 cudaError_t launch_backward(const BackParams &p, bool fast, float *dw, int accumulate, cudaStream_t stream) {
-  const Shape sh = shape_of(p.H, true);
+  const Shape sh = shape_of(p.H);
   int rows;
   if (fast && sh.per) {
-    const int grid = backward_blocks(p.T, sh.rpb), block = sh.tpr * sh.rpb;
-    rows = grid * sh.rpb;
+    const int block = sh.tpr * sh.rpb;
+    static std::atomic<int> known[5][33];
+    const auto go = [&](auto kernel) {
+      const int grid = backward_blocks(p.T, sh.rpb, resident(kernel, known[sh.per], block, sm_count()));
+      rows = grid * sh.rpb;
+      kernel<<<grid, block, 0, stream>>>(p, sh.tpr);
+    };
     if (sh.per == 1)
-      rms_norm_backward_kernel<T, TD, 1><<<grid, block, 0, stream>>>(p, sh.tpr);
+      go(rms_norm_backward_kernel<T, TD, 1>);
     else if (sh.per == 2)
-      rms_norm_backward_kernel<T, TD, 2><<<grid, block, 0, stream>>>(p, sh.tpr);
+      go(rms_norm_backward_kernel<T, TD, 2>);
     else
-      rms_norm_backward_kernel<T, TD, 4><<<grid, block, 0, stream>>>(p, sh.tpr);
+      go(rms_norm_backward_kernel<T, TD, 4>);
   } else {
-    rows = backward_blocks(p.T, 1);
+    rows = backward_blocks(p.T, 1, kMaxPartials);
     rms_norm_backward_any_kernel<T, TD><<<rows, kAnyThreads, 0, stream>>>(p);
   }
   cudaError_t e = cudaGetLastError();

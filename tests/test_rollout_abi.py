@@ -122,7 +122,7 @@ def test_product_refusals(lib):
                 a_scale=0x3000, b_scale=0x4000, c=0x5000, status=0x6000)
     _refused(fn, b.GemmFp8Args, good, [
         (bad, dict(struct_size=0)), (bad, dict(M=-1)), (bad, dict(N=-1)), (bad, dict(K=0)), (bad, dict(launch_hint=3)),
-        (bad, dict(launch_hint=2, M=129)), (bad, dict(a=None)), (bad, dict(b=None)), (bad, dict(a_scale=None)),
+        (bad, dict(launch_hint=2, M=65)), (bad, dict(a=None)), (bad, dict(b=None)), (bad, dict(a_scale=None)),
         (bad, dict(b_scale=None)), (bad, dict(c=None)), (bad, dict(status=None)), (bad, dict(lda=192)), (bad, dict(ldb=192)),
         (bad, dict(ldc=299)), (bad, dict(ld_a_scale=1)), (bad, dict(ld_b_scale=1)), (unsupported, dict(c_dtype=b.DVP_E4M3)),
         (unsupported, dict(lda=200)), (unsupported, dict(ldb=200)), (unsupported, dict(a=0x1008)), (unsupported, dict(b=0x2004)),
