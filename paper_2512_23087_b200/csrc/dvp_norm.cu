@@ -86,7 +86,7 @@ __device__ __forceinline__ void load_weights8(const void *w, int w_f32, long lon
 }
 template <typename T>
 __device__ __forceinline__ float load_weight(const void *w, int w_f32, long long c) {
-  return sizeof(T) == 4 || w_f32 ? static_cast<const float *>(w)[c] : Storage<T>::widen(static_cast<const T *>(w)[c]);
+  return sizeof(T) == 4 || w_f32 ? __ldg(static_cast<const float *>(w) + c) : Storage<T>::widen(__ldg(static_cast<const T *>(w) + c));
 }
 
 __device__ __forceinline__ uint32_t fp8_pair(float lo, float hi) {
@@ -107,64 +107,97 @@ __device__ __forceinline__ float row_sum(float v, int tpr, float *part) {
   const int warp = threadIdx.x >> 5, warps = tpr >> 5, first = warp / warps * warps;
   if ((threadIdx.x & 31) == 0) part[warp] = v;
   __syncthreads();
+  if (warps == 8 || warps == 16) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      if (i >= warps) break;
+      const float4 q = *reinterpret_cast<const float4 *>(part + first + i);
+      s += (q.x + q.y) + (q.z + q.w);
+    }
+    return s;
+  }
   float s = 0.f;
   for (int i = 0; i < warps; ++i) s += part[first + i];
   return s;
 }
 
+// Reciprocals and roots as the special-function unit gives them, to 2^-22.
+__device__ __forceinline__ float approx_rcp(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // ---- rows in vectors ---------------------------------------------------------------------------------------------------
 
 // A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: the next is on its way while one is summed up and stored, so that loads
-// never pause (16,384 x 4,096 bfloat16 to 8 bits: FWD_NOW us, with one row a block and nothing on its way 139).
+// never pause (16,384 x 4,096 bfloat16 to 8 bits: 103 us, with one row a block and nothing on its way 139).
 template <typename T, typename TOut, int kPer>
-__global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rms_norm_kernel(const Params p, const int tpr) {
-  __shared__ float part[2][32];
+__global__ void __launch_bounds__(kPer == 4 ? 512 : 256, kPer == 1 ? 4 : kPer == 2 ? 3 : 1) rms_norm_kernel(const Params p, const int tpr) {
+  __shared__ __align__(16) float part[2][32];
   const int lane_of_row = threadIdx.x % tpr, rpb = blockDim.x / tpr;
   const long long step = (long long)gridDim.x * rpb;
-  Raw<T> x[kPer], r[kPer];
+  // rows on their way: two where their registers are few
+  constexpr int kAhead = kPer == 1 && sizeof(T) == 2 ? 2 : 1;
+  Raw<T> x[kAhead][kPer], r[kAhead][kPer];
   const auto column = [&](int i) { return ((long long)lane_of_row + (long long)i * tpr) * kVec; };
-  const auto fetch = [&](long long t) {
+  long long t = (long long)blockIdx.x * rpb + threadIdx.x / tpr;
+  // the row to fetch next, and this one's outputs, at the thread's first column
+  const T *x_at = static_cast<const T *>(p.x) + t * p.ld_x + column(0), *r_at = static_cast<const T *>(p.r) + t * p.ld_r + column(0);
+  T *h_at = static_cast<T *>(p.r_out) + t * p.ld_r_out + column(0);
+  TOut *y_at = static_cast<TOut *>(p.out) + t * p.ld_out + column(0);
+  bool in[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) in[i] = column(i) < p.H;
+  const bool has_r = p.r != nullptr, has_h = p.r_out != nullptr;
+  const int across = tpr * kVec;
+  const auto fetch = [&](Raw<T> (&x)[kPer], Raw<T> (&r)[kPer], bool live) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const long long c = column(i);
-      if (t < p.T && c < p.H) {
-        x[i].load(static_cast<const T *>(p.x) + t * p.ld_x + c);
-        if (p.r) r[i].load(static_cast<const T *>(p.r) + t * p.ld_r + c);
+      if (live && in[i]) {
+        x[i].load(x_at + i * across);
+        if (has_r) r[i].load(r_at + i * across);
       } else {
         x[i].zero();
         r[i].zero();
       }
     }
+    x_at += step * p.ld_x;
+    r_at += step * p.ld_r;
   };
-  long long t = (long long)blockIdx.x * rpb + threadIdx.x / tpr;
-  fetch(t);
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) fetch(x[a], r[a], t + a * step < p.T);
   int turn = 0;
   for (long long first = (long long)blockIdx.x * rpb; first < p.T; first += step, t += step, turn ^= 1) {
     const bool live = t < p.T;
     float h[kPer][kVec], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      x[i].widen(h[i]);
-      if (p.r) {
+      x[0][i].widen(h[i]);
+      if (has_r) {
         float v[kVec];
-        r[i].widen(v);
+        r[0][i].widen(v);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) h[i][j] += v[j];
       }
 #pragma unroll
       for (int j = 0; j < kVec; ++j) sum = fmaf(h[i][j], h[i][j], sum);
     }
-    if (first + step < p.T) fetch(t + step);
-    const float s = 1.f / sqrtf(fmaf(row_sum(sum, tpr, part[turn]), p.inv_h, p.eps));  // two sets: see the backward kernel
+#pragma unroll
+    for (int a = 0; a + 1 < kAhead; ++a)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) x[a][i] = x[a + 1][i], r[a][i] = r[a + 1][i];
+    if (first + kAhead * step < p.T) fetch(x[kAhead - 1], r[kAhead - 1], t + kAhead * step < p.T);
+    const float s = rsqrtf(fmaf(row_sum(sum, tpr, part[turn]), p.inv_h, p.eps));  // two sets: see the backward kernel
     if (live && lane_of_row == 0 && p.rstd) p.rstd[t] = s;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const long long c = column(i);
-      const bool here = live && c < p.H;
-      if (p.r_out && here) store8(static_cast<T *>(p.r_out) + t * p.ld_r_out + c, h[i]);
+      const bool here = live && in[i];
+      if (has_h && here) store8(h_at + i * across, h[i]);
       float w[kVec], y[kVec];
       if (here) {
-        load_weights8<T>(p.w, p.w_f32, c, w);
+        load_weights8<T>(p.w, p.w_f32, column(i), w);
       } else {
 #pragma unroll
         for (int j = 0; j < kVec; ++j) w[j] = 0.f;
@@ -178,18 +211,20 @@ __global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rms_norm_kernel(con
         for (int j = 0; j < kVec; ++j) a = fmaxf(a, fabsf(y[j]));
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        const float scale = a / kFp8Max, inv = 1.f / scale;
+        const float scale = a * (1.f / kFp8Max), inv = approx_rcp(scale);
         if (here) {
-          if ((threadIdx.x & 15) == 0) p.scale[t * p.ld_scale + c / kBlockCols] = scale;
+          if ((threadIdx.x & 15) == 0) p.scale[t * p.ld_scale + column(i) / kBlockCols] = scale;
           uint2 q;
           q.x = fp8_pair(y[0] * inv, y[1] * inv) | fp8_pair(y[2] * inv, y[3] * inv) << 16;
           q.y = fp8_pair(y[4] * inv, y[5] * inv) | fp8_pair(y[6] * inv, y[7] * inv) << 16;
-          st_stream8(static_cast<uint8_t *>(p.out) + t * p.ld_out + c, q);
+          st_stream8(y_at + i * across, q);
         }
       } else if (here) {
-        store8(static_cast<TOut *>(p.out) + t * p.ld_out + c, y);
+        store8(y_at + i * across, y);
       }
     }
+    h_at += step * p.ld_r_out;
+    y_at += step * p.ld_out;
   }
 }
 
@@ -209,48 +244,49 @@ __device__ __forceinline__ float block_sum(float v, float *part) {
 }
 
 // A warp takes whole blocks of 128 columns, four a lane, in both sweeps alike: what takes an input's place is written by the
-// thread that has read it last.
+// thread that has read it last.  (Kept in registers between the sweeps, 32 a thread, the rows were slower: 1,111 x 5,003 float16 16.4 us
+// a call, read twice 12.3, as twice as many blocks fit an SM.)
 template <typename T, typename TOut>
 __global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params p) {
   __shared__ float part[kAnyThreads / 32];
+  constexpr int kWarps = kAnyThreads / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long blocks = (p.H + kBlockCols - 1) / kBlockCols;
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
     const T *x = static_cast<const T *>(p.x) + t * p.ld_x;
     const T *r = p.r ? static_cast<const T *>(p.r) + t * p.ld_r : nullptr;
     const auto entry = [&](long long c) { return Storage<T>::widen(x[c]) + (r ? Storage<T>::widen(r[c]) : 0.f); };
+    const auto column = [&](long long b, int j) { return b * kBlockCols + j * 32 + lane; };
     float sum = 0.f;
-    for (long long b = warp; b < blocks; b += kAnyThreads / 32)
+    for (long long b = warp; b < blocks; b += kWarps)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const long long c = b * kBlockCols + j * 32 + lane;
+        const long long c = column(b, j);
         const float v = c < p.H ? entry(c) : 0.f;
         sum = fmaf(v, v, sum);
       }
-    const float s = 1.f / sqrtf(fmaf(block_sum(sum, part), p.inv_h, p.eps));
+    const float s = rsqrtf(fmaf(block_sum(sum, part), p.inv_h, p.eps));
     if (threadIdx.x == 0 && p.rstd) p.rstd[t] = s;
-    for (long long b = warp; b < blocks; b += kAnyThreads / 32) {
+    for (long long b = warp; b < blocks; b += kWarps) {
       float h[4], y[4], a = kLeastAmax;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const long long c = b * kBlockCols + j * 32 + lane;
-        h[j] = y[j] = 0.f;
-        if (c < p.H) {
-          h[j] = entry(c);
-          y[j] = h[j] * s * load_weight<T>(p.w, p.w_f32, c);
-        }
+        const long long c = column(b, j);
+        h[j] = c < p.H ? entry(c) : 0.f;
+        y[j] = c < p.H ? h[j] * s * load_weight<T>(p.w, p.w_f32, c) : 0.f;
         a = fmaxf(a, fabsf(y[j]));
       }
-      float scale = 1.f, inv = 1.f;
+      float inv = 1.f;
       if constexpr (sizeof(TOut) == 1) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        scale = a / kFp8Max, inv = 1.f / scale;
+        const float scale = a * (1.f / kFp8Max);
+        inv = approx_rcp(scale);
         if (lane == 0) p.scale[t * p.ld_scale + b] = scale;
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const long long c = b * kBlockCols + j * 32 + lane;
+        const long long c = column(b, j);
         if (c >= p.H) continue;
         if (p.r_out) static_cast<T *>(p.r_out)[t * p.ld_r_out + c] = Storage<T>::narrow(h[j]);
         if constexpr (sizeof(TOut) == 1)
@@ -276,8 +312,8 @@ struct BackParams {
 
 // A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: its threads keep their columns, and with them the sums of dw.
 template <typename T, typename TD, int kPer>
-__global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rms_norm_backward_kernel(const BackParams p, const int tpr) {
-  __shared__ float part[2][32];
+__global__ void __launch_bounds__(512, kPer == 1 ? 2 : 1) rms_norm_backward_kernel(const BackParams p, const int tpr) {
+  __shared__ __align__(16) float part[2][32];
   const int lane_of_row = threadIdx.x % tpr, rpb = blockDim.x / tpr, row_of_block = threadIdx.x / tpr;
   float w[kPer][kVec], dw[kPer][kVec];
 #pragma unroll
@@ -416,9 +452,9 @@ struct Shape {
   int per, tpr, rpb;  // vectors a thread, threads a row, rows a block
 };
 // One vector a thread up to 512 threads a row, then more.  per = 0: too long for the registers, or no vector at all.
-inline Shape shape_of(long long H) {
+inline Shape shape_of(long long H, bool backward) {
   const long long nv = H / kVec;
-  const int per = nv < 1 ? 0 : nv <= 512 ? 1 : nv <= 1024 ? 2 : nv <= 2048 ? 4 : 0;
+  const int per = nv < 1 ? 0 : nv <= (backward ? 512 : 256) ? 1 : nv <= (backward ? 1024 : 512) ? 2 : nv <= 2048 ? 4 : 0;
   if (!per) return {0, 0, 0};
   const int tpr = (int)(((nv + per - 1) / per + 31) / 32 * 32);
   return {per, tpr, tpr >= 256 ? 1 : 256 / tpr};
@@ -449,7 +485,7 @@ cudaError_t by_type(int d, F f) {
 
 template <typename T, typename TOut>
 cudaError_t launch_forward(const Params &p, bool fast, cudaStream_t stream) {
-  const Shape sh = shape_of(p.H);
+  const Shape sh = shape_of(p.H, false);
   if (fast && sh.per) {
     const int block = sh.tpr * sh.rpb;
     const long long want = (p.T + sh.rpb - 1) / sh.rpb;
@@ -479,7 +515,7 @@ inline int backward_blocks(long long T, int rpb, int most_blocks) {
 
 template <typename T, typename TD>
 cudaError_t launch_backward(const BackParams &p, bool fast, float *dw, int accumulate, cudaStream_t stream) {
-  const Shape sh = shape_of(p.H);
+  const Shape sh = shape_of(p.H, true);
   int rows;
   if (fast && sh.per) {
     const int block = sh.tpr * sh.rpb;

@@ -295,6 +295,35 @@ at::ScalarType type_of(PyObject *o) {
 at::Tensor make(const at::Tensor &like, at::IntArrayRef sizes, at::ScalarType type) {
   return at::empty(sizes, like.options().dtype(type).requires_grad(false));
 }
+// Tensors that a call makes: of a small call all over one storage, since an allocation takes longer than its part of the kernel; of
+// larger ones each by itself, so that keeping one keeps nothing else.
+struct Outputs {
+  static constexpr int64_t kSmall = 1 << 20;
+  const at::Tensor &like;
+  at::Tensor buf;
+  int64_t at = 0;
+  Outputs(const at::Tensor &like_, int64_t bytes) : like(like_) {
+    if (bytes <= kSmall) buf = ::make(like, {bytes}, at::kByte);
+  }
+  static int64_t room(int64_t rows, int64_t cols, at::ScalarType type) {
+    return (rows * cols * static_cast<int64_t>(c10::elementSize(type)) + 255) / 256 * 256;
+  }
+  // [rows, cols] of rows of `ld` elements; cols < 0: a vector
+  at::Tensor take(int64_t rows, int64_t cols, int64_t ld, at::ScalarType type) {
+    if (!buf.defined()) {
+      at::Tensor t = cols < 0 ? ::make(like, {rows}, type) : ::make(like, {rows, ld}, type);
+      return cols >= 0 && cols != ld ? t.narrow(1, 0, cols) : t;
+    }
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(buf.storage()), buf.key_set(), c10::scalarTypeToTypeMeta(type));
+    impl->set_storage_offset(at / static_cast<int64_t>(c10::elementSize(type)));
+    if (cols < 0)
+      impl->set_sizes_contiguous({rows});
+    else
+      impl->set_sizes_and_strides(at::IntArrayRef({rows, cols}), at::IntArrayRef({ld, int64_t(1)}));
+    at += room(rows, cols < 0 ? 1 : ld, type);
+    return at::Tensor(std::move(impl));
+  }
+};
 PyObject *finish(int status, THPObjectPtr &result) { return status == DVP_OK ? result.release() : PyLong_FromLong(status); }
 
 // rms_norm(entry, x, weight, residual, eps, out_dtype, residual_out, stream)
@@ -327,25 +356,22 @@ PyObject *rms_norm(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     const at::Tensor &r = like_matrix(args[3], "residual", x);
     a.residual = r.data_ptr(), a.ld_residual = r.stride(0);
   }
-  if (given(args[6]))
-    h = like_matrix(args[6], "residual_out", x);
-  else if (given(args[3]))
-    h = make(x, {T, H}, x.scalar_type());
-  if (h.defined()) a.residual_out = h.data_ptr(), a.ld_residual_out = h.stride(0);
+  if (given(args[6])) h = like_matrix(args[6], "residual_out", x);
   const bool fp8 = a.out_dtype == DVP_E4M3;
   // 8-bit rows start on 16-byte boundaries, where the tensor cores' loads want them
-  at::Tensor y = fp8 ? make(x, {T, (H + 15) / 16 * 16}, out) : make(x, {T, H}, out);
-  a.out = y.data_ptr(), a.ld_out = y.stride(0);
-  if (fp8 && y.size(1) != H) y = y.narrow(1, 0, H);
-  // rstd and the scales over one storage
-  const int64_t blocks = (H + 127) / 128, rows = (T + 3) / 4 * 16;
-  const at::Tensor buf = make(x, {rows + (fp8 ? T * blocks * 4 : 0)}, at::kByte);
-  a.rstd = static_cast<float *>(buf.data_ptr());
-  const at::Tensor rstd = row_view(buf.storage(), buf.key_set(), at::kFloat, 0, rows, T);
+  const int64_t ld = fp8 ? (H + 15) / 16 * 16 : H, blocks = (H + 127) / 128;
+  const bool make_h = !h.defined() && given(args[3]);
+  Outputs made(x, Outputs::room(T, ld, out) + Outputs::room(T, 1, at::kFloat) + (fp8 ? Outputs::room(T, blocks, at::kFloat) : 0) +
+                      (make_h ? Outputs::room(T, H, x.scalar_type()) : 0));
+  if (make_h) h = made.take(T, H, H, x.scalar_type());
+  if (h.defined()) a.residual_out = h.data_ptr(), a.ld_residual_out = h.stride(0);
+  const at::Tensor y = made.take(T, H, ld, out), rstd = made.take(T, -1, 0, at::kFloat);
+  a.out = y.data_ptr(), a.ld_out = ld;
+  a.rstd = static_cast<float *>(rstd.data_ptr());
   if (fp8) {
-    a.scale = reinterpret_cast<float *>(static_cast<char *>(buf.data_ptr()) + rows);
-    a.ld_scale = blocks;
-    put(d.get(), g_more.scale, THPVariable_Wrap(row_view(buf.storage(), buf.key_set(), at::kFloat, 1, rows, T * blocks).view({T, blocks})));
+    const at::Tensor scale = made.take(T, blocks, blocks, at::kFloat);
+    a.scale = static_cast<float *>(scale.data_ptr()), a.ld_scale = blocks;
+    put(d.get(), g_more.scale, THPVariable_Wrap(scale));
   } else {
     put(d.get(), g_more.scale, none());
   }
@@ -388,10 +414,11 @@ PyObject *rms_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args
   }
   a.accumulate_dw = PyObject_IsTrue(args[8]);
   if (a.accumulate_dw && !given(args[7])) refuse(PyExc_ValueError, "%s needs d_weight", "accumulate_dw");
-  const at::Tensor d_weight = given(args[7]) ? vector(args[7], "d_weight", H, at::kFloat, at::kFloat, h) : make(h, {H}, at::kFloat);
+  Outputs made(h, Outputs::room(T, H, h.scalar_type()) + Outputs::room(H, 1, at::kFloat));
+  const at::Tensor d_x = made.take(T, H, H, h.scalar_type());
+  a.d_x = d_x.data_ptr(), a.ld_d_x = H;
+  const at::Tensor d_weight = given(args[7]) ? vector(args[7], "d_weight", H, at::kFloat, at::kFloat, h) : made.take(H, -1, 0, at::kFloat);
   a.d_weight = static_cast<float *>(d_weight.data_ptr());
-  const at::Tensor d_x = make(h, {T, H}, h.scalar_type());
-  a.d_x = d_x.data_ptr(), a.ld_d_x = d_x.stride(0);
   at::Tensor workspace;
   if (given(args[9])) {
     workspace = tensor(args[9], "workspace");
