@@ -452,6 +452,38 @@ struct Row {
     return mask;
   }
 
+  // Of the warp's pieces i0 to i0 + 31 those with a granule that reaches `v`: a bit each.
+  __device__ __forceinline__ unsigned hot_pieces(int i0, float v) const {
+    const int n = min(32, mine - i0);
+    if (!bounded) return n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+    const uint16_t *b = bounds() + (first + i0) * 32 + lane;
+    unsigned hot = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i)
+      if (__any_sync(0xffffffffu, __uint_as_float((uint32_t)b[i * 32] << 16) >= v)) hot |= 1u << i;
+    return hot;
+  }
+  // Calls f(i, w) for the warp's pieces with a granule that reaches `v`, the next one's load under way; of every 32 those in `of`.
+  template <typename F>
+  __device__ __forceinline__ void each_hot(float v, F f, unsigned of = 0xffffffffu) const {
+#pragma unroll 1
+    for (int i0 = 0; i0 < mine; i0 += 32) {
+      unsigned hot = hot_pieces(i0, v) & of;
+      uint32_t next[8];
+      if (hot) load(first + i0 + __ffs(hot) - 1, next);
+#pragma unroll 1
+      while (hot) {
+        const int i = i0 + __ffs(hot) - 1;
+        hot &= hot - 1;
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = next[j];
+        if (hot) load(first + i0 + __ffs(hot) - 1, next);
+        f(i, w);
+      }
+    }
+  }
+
   // What a pass over the row looks for: the logits above `v`, those equal to it up to index `i`, none above `most`.  Of these the
   // ones above `split` are summed up; the others go where `rest` says.
   enum Rest { kNone, kFirst, kBinsOfKeys, kToList };
@@ -478,50 +510,27 @@ struct Row {
   __device__ __noinline__ static Sum pass(Row row, const Pass a) {
     float *value = sh()->compact.value[row.warp];
     uint16_t *place = sh()->compact.place[row.warp];
-    double acc = 0.0, of_part = 0.0;
+    double acc = 0.0;
     double *parts = sh()->part[row.warp];
     int n = 0, best = kNoIndex;
-    const auto hot = [&](int i) {
-      return i < row.mine &&
-             (!row.bounded || __uint_as_float((uint32_t)bounds()[(row.first + i) * 32 + row.lane] << 16) >= a.v);
-    };
     const bool plain = a.i == kNoIndex && a.most == -kNegInf;
-    uint32_t next[8];
-    bool next_hot = hot(0);
-    if (next_hot) row.load(row.first, next);
-#pragma unroll 1
-    for (int i = 0; i < row.mine; ++i) {
-      uint32_t w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = next[j];
-      const bool here = next_hot;
-      next_hot = hot(i + 1);
-      if (next_hot) row.load(row.first + i + 1, next);
+    for (int q = row.lane; q < kParts; q += 32) parts[q] = 0.0;
+    __syncwarp();
+    row.each_hot(a.v, [&](int i, const uint32_t (&w)[8]) {
       const int i0 = row.first_of(row.first + i), base = i0 - row.lane * kPer;
-      unsigned mask = 0;
-      if (here) {
-        mask = from(w, a.v);
-        if (!plain) {
+      unsigned mask = from(w, a.v);
+      if (!plain) {
 #pragma unroll
-          for (int j = 0; j < kPer / 2; ++j) {
-            float lo, hi;
-            two_of<T>(w, j, lo, hi);
-            if (!(lo <= a.most && (lo > a.v || i0 + 2 * j <= a.i))) mask &= ~(1u << (2 * j));
-            if (!(hi <= a.most && (hi > a.v || i0 + 2 * j + 1 <= a.i))) mask &= ~(2u << (2 * j));
-          }
+        for (int j = 0; j < kPer / 2; ++j) {
+          float lo, hi;
+          two_of<T>(w, j, lo, hi);
+          if (!(lo <= a.most && (lo > a.v || i0 + 2 * j <= a.i))) mask &= ~(1u << (2 * j));
+          if (!(hi <= a.most && (hi > a.v || i0 + 2 * j + 1 <= a.i))) mask &= ~(2u << (2 * j));
         }
       }
-      const bool ends = ((i + 1) & ((1 << row.log_q) - 1)) == 0 || i + 1 == row.mine;
-      if (!__any_sync(0xffffffffu, mask != 0)) {
-        if (ends) {
-          if (row.log_q > 0) of_part = warp_sum(of_part);
-          if (row.lane == 0) parts[i >> row.log_q] = of_part;
-          acc += of_part;
-          of_part = 0.0;
-        }
-        continue;
-      }
+      if (!__any_sync(0xffffffffu, mask != 0)) return;
       const int own = __popc(mask), up_to = warp_scan(own), all = __shfl_sync(0xffffffffu, up_to, 31);
+      double of_piece = 0.0;
       int at = up_to - own;
       if (a.rest == kNone) {
         // sums alone: two side by side, as one exponential is a long chain
@@ -534,12 +543,12 @@ struct Row {
         }
         __syncwarp();
         if (!a.weights) {
-          of_part += (double)own;
+          of_piece += (double)own;
         } else {
 #pragma unroll 1
           for (int e = row.lane; e < all; e += 64) {
             const double one = row.weight(value[e]), two = row.weight(e + 32 < all ? value[e + 32] : kNegInf);
-            of_part += one + two;
+            of_piece += one + two;
           }
         }
         n += own;
@@ -562,7 +571,7 @@ struct Row {
         for (int e = row.lane; e < all; e += 32) {
           const float v = value[e];
           if (v > a.split) {
-            of_part += a.weights ? row.weight(v) : 1.0;
+            of_piece += a.weights ? row.weight(v) : 1.0;
             ++n;
           } else {
             const int at_row = base + place[e];
@@ -577,13 +586,14 @@ struct Row {
         }
       }
       __syncwarp();
-      if (ends) {
-        of_part = warp_sum(of_part);
-        if (row.lane == 0) parts[i >> row.log_q] = of_part;
-        acc += of_part;
-        of_part = 0.0;
+      if (a.rest != kFirst && a.rest != kBinsOfKeys) {
+        of_piece = warp_sum(of_piece);
+        if (row.lane == 0) parts[i >> row.log_q] += of_piece;
+        acc += of_piece;
+      } else if (__any_sync(0xffffffffu, of_piece != 0.0)) {
+        acc += warp_sum(of_piece);
       }
-    }
+    });
     const bool first = a.rest == kFirst;
     n = first ? __reduce_min_sync(0xffffffffu, best) : __reduce_add_sync(0xffffffffu, n);
     __syncthreads();  // chunk and warp_n have been read
@@ -613,25 +623,11 @@ struct Row {
     return r;
   }
   // The histogram of the distances of what is kept, none below `low`: most of a row's logits, one by one.
-  __device__ __noinline__ static void bins_of_distance(Row row, float low, float per) {
+  __device__ __noinline__ static void bins_of_distance(Row row, float low, float per, unsigned of) {
     uint32_t *hist = row.sh()->hist;
-    const auto hot = [&](int i) {
-      return i < row.mine && (!row.bounded || __uint_as_float((uint32_t)bounds()[(row.first + i) * 32 + row.lane] << 16) >= low);
-    };
     const bool plain = low > row.cut_v || row.cut_i == kNoIndex;
     const float v = fmaxf(low, row.cut_v);
-    uint32_t next[8];
-    bool next_hot = hot(0);
-    if (next_hot) row.load(row.first, next);
-#pragma unroll 1
-    for (int i = 0; i < row.mine; ++i) {
-      uint32_t w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = next[j];
-      const bool here = next_hot;
-      next_hot = hot(i + 1);
-      if (next_hot) row.load(row.first + i + 1, next);
-      if (!here) continue;
+    row.each_hot(v, [&](int i, const uint32_t (&w)[8]) {
       const int i0 = row.first_of(row.first + i);
 #pragma unroll
       for (int j = 0; j < kPer / 2; ++j) {
@@ -640,7 +636,7 @@ struct Row {
         if (lo >= v && (plain || row.kept(lo, i0 + 2 * j))) atomicAdd(&hist[row.bin_of(lo, per)], 1u);
         if (hi >= v && (plain || row.kept(hi, i0 + 2 * j + 1))) atomicAdd(&hist[row.bin_of(hi, per)], 1u);
       }
-    }
+    }, of);
   }
   // The sum of the warps' parts that lie in `chunk`.
   __device__ __forceinline__ double sum_of_chunks() {
@@ -782,13 +778,13 @@ struct Row {
       uint32_t lo = 0, hi = 0xffff;  // of the order: the largest b that k bounds reach
       for (int round = 0; lo < hi; ++round) {
         const uint32_t mid = (lo + hi + 1) >> 1;
-        // of the order, and so of the values: bounds of the least such value and above
+        // of the order, and so of the values: bounds of the least such value and above, two at a time
         const float v = value_of(mid << 16 | (mid & 0x8000u ? 0u : 0xffffu));
-        int reach = 0;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-          const uint32_t two = pairs[i];
-          reach += (__uint_as_float(two << 16) >= v) + (__uint_as_float(two & 0xffff0000u) >= v);
-        }
+        __nv_bfloat162 least;
+        least.x = least.y = __ushort_as_bfloat16((unsigned short)(__float_as_uint(v) >> 16));
+        int two = 0;
+        for (int i = threadIdx.x; i < n; i += kThreads) two += __hge2_mask(reinterpret_cast<const __nv_bfloat162 &>(pairs[i]), least) & 0x10001u;
+        int reach = (two & 0xffff) + (two >> 16);
         reach = __reduce_add_sync(0xffffffffu, reach);
         // three counters in turn: one is added to, one is read, one is cleared for the next
         if (lane == 0 && reach) atomicAdd(&sh()->counter[round % 3], (uint32_t)reach);
@@ -821,9 +817,23 @@ struct Row {
     // level 0: bins of distance; from level 1 on logits from `low` to `high`, in bins by their keys
     float low = floor, high = m;
     uint32_t n_in = 0;
+    // A histogram of all that can matter costs more than reading the row again.  Where a warp has pieces enough, one of an eighth
+    // of them guesses where the cut is, and what is found there shows whether it was right.
+    bool guess = unsure > 0.0 && all_segs >= 16 * kWarps * blocks;
+    if (guess) {
+      for (int i = threadIdx.x; i < kBins; i += kThreads) sh()->hist[i] = 0;
+      __syncthreads();
+      bins_of_distance(*this, low, per, 0x01010101u << (warp & 7));
+      meet();
+      window((1.0 - share) * all, below, per);
+      n_in = sh()->pick_last;
+      guess = n_in <= kList * 7 / 8 && per > 0.f;
+      if (guess) edges(sh()->pick_lo, sh()->pick_hi, per, low, high);
+      meet();  // the histograms have been read
+    }
     // every level divides the keys by 2,048, at the latest from the eighth on: eleven are the most
 #pragma unroll 1
-    for (int level = 0; level < 16; ++level) {
+    for (int level = guess ? 1 : 0; level < 16; ++level) {
       const uint32_t k_lo = key_of(low), k_hi = key_of(high), width = k_hi - k_lo;
       const int shift = max(0, 21 - __clz(width));  // (width >> shift) < kBins
       const bool gather = level > 0 && n_in <= kList;
@@ -848,7 +858,7 @@ struct Row {
       Sum above = {0.0, 0};
       double tail = 0.0;
       if (level == 0) {
-        bins_of_distance(*this, low, per);
+        bins_of_distance(*this, low, per, 0xffffffffu);
         meet();
       } else if (gather && unsure > 0.0) {
         tail = behind(low, high);
@@ -887,13 +897,21 @@ struct Row {
           n += k;
         }
         if (blocks > 1) meet();  // the lists have been read
-        if (n > kList) {         // more on the bracket's edge than its bins had
+        if (n > kList && !guess) {  // more on the bracket's edge than its bins had
           n_in = (uint32_t)n;
           continue;
         }
-        sort_list(n);
+        if (n <= kList) sort_list(n);
         int last;
-        if (unsure > 0.0) {
+        if (guess) {
+          const double end = (1.0 - share) * all;
+          if (n > kList || !cut_from_list(true, n, tail - end, true, (1.0 - share) * unsure + tail * eps(tail), last)) {
+            guess = false;  // the long way then
+            low = floor, high = m;
+            level = -1;
+            continue;
+          }
+        } else if (unsure > 0.0) {
           // Kept is what has more than (1 - share) all at and behind it.  Of that side's sums, the whole's and the tail's, float32's
           // errors are the smaller by 1 - share; mostly nothing lies so near the border that they matter.
           const double end = (1.0 - share) * all;
@@ -921,15 +939,88 @@ struct Row {
       meet();  // the histograms have been read
       if (n_in == 0) return;  // less than the aim in all: everything stays
       if (level == 0) {
-        // the values that the bins' logits can have; 2^-20 covers the roundings of the distance
-        const double slack = 9.5367431640625e-7;
-        if (per > 0.f) {
-          high = fminf(m, __double2float_ru((double)m - (double)lo / per * (1.0 - slack)));
-          if (hi < kBins - 1) low = fmaxf(low, __double2float_rd((double)m - ((double)hi + 1.0) / per * (1.0 + slack)));
-        }
+        edges(lo, hi, per, low, high);
       } else {
         low = fmaxf(low, value_of(edge_of(k_lo, k_hi, hi, shift)));
         high = value_of(k_hi - (lo << shift));
+      }
+    }
+  }
+  // The values, from low to high, that the logits in bins lo to hi can have; 2^-20 covers the roundings of the distance.
+  __device__ __forceinline__ void edges(uint32_t lo, uint32_t hi, float per, float &low, float &high) const {
+    const double slack = 9.5367431640625e-7;
+    if (!(per > 0.f)) return;
+    high = fminf(m, __double2float_ru((double)m - (double)lo / per * (1.0 - slack)));
+    if (hi < kBins - 1) low = fmaxf(low, __double2float_rd((double)m - ((double)hi + 1.0) / per * (1.0 + slack)));
+  }
+  // From the histograms of an eighth of the row: the bins in which the sum over what lies behind can fall below `end`, within four
+  // standard deviations and 2 %: pick_lo to pick_hi, which may have pick_last logits.  Every block alike.
+  __device__ void window(double end, double below, float per) {
+    constexpr int kOwn = kBins / kThreads;
+    uint32_t n[kOwn];
+    float w[kOwn], sum = 0.f, squares = 0.f;
+    bins_of_row(n);
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      w[j] = ex2(-((float)(threadIdx.x * kOwn + j) + 0.5f) / per * c);
+      sum += (float)n[j] * w[j];
+      squares += (float)n[j] * w[j] * w[j];
+    }
+    const float sum_up = warp_scan(sum), squares_up = warp_scan(squares);
+    __syncthreads();
+    if (lane == 31) {
+      sh()->warp_a[warp] = (double)sum_up;
+      sh()->warp_b[warp] = (double)squares_up;
+    }
+    if (threadIdx.x == 0) sh()->pick_lo = sh()->pick_hi = kBins - 1;
+    __syncthreads();
+    // what lies behind this thread's bins: all, less what lies in front of them and in them
+    float behind_w = 0.f, behind_s = 0.f;
+    for (int v = warp; v < kWarps; ++v) behind_w += (float)sh()->warp_a[v], behind_s += (float)sh()->warp_b[v];
+    behind_w -= sum_up - sum;
+    behind_s -= squares_up - squares;
+    uint32_t lo = kBins, hi = kBins;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      behind_w -= (float)n[j] * w[j];
+      behind_s -= (float)n[j] * w[j] * w[j];
+      const float off = 4.f * sqrtf(56.f * fmaxf(behind_s, 0.f)) + 0.02f * (float)end + (float)below;
+      if (8.f * behind_w - off < (float)end) lo = min(lo, threadIdx.x * kOwn + j);
+      if (8.f * behind_w + off < (float)end) hi = min(hi, threadIdx.x * kOwn + j);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_min_sync(0xffffffffu, hi);
+    if (lane == 0) {
+      if (lo < (uint32_t)kBins) atomicMin(&sh()->pick_lo, lo);
+      if (hi < (uint32_t)kBins) atomicMin(&sh()->pick_hi, hi);
+    }
+    __syncthreads();
+    lo = sh()->pick_lo, hi = sh()->pick_hi;
+    uint32_t inside = 0;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      const uint32_t b = threadIdx.x * kOwn + j;
+      if (b >= lo && b <= hi) inside += n[j];
+    }
+    inside = __reduce_add_sync(0xffffffffu, inside);
+    if (threadIdx.x == 0) sh()->pick_last = 0;
+    __syncthreads();
+    if (lane == 0 && inside) atomicAdd(&sh()->pick_last, 8 * inside);
+    __syncthreads();
+  }
+  // The row's numbers in the thread's bins.
+  __device__ __forceinline__ void bins_of_row(uint32_t (&n)[kBins / kThreads]) const {
+    constexpr int kOwn = kBins / kThreads;
+    static_assert(kOwn % 4 == 0, "bins are read four at a time");
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) n[j] = 0;
+#pragma unroll 1
+    for (int r = 0; r < blocks; ++r) {
+      const uint32_t *hist = (r ? of((rank + r) & (blocks - 1)) : sh())->hist + threadIdx.x * kOwn;
+#pragma unroll
+      for (int j = 0; j < kOwn; j += 4) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(hist + j);
+        n[j] += q.x, n[j + 1] += q.y, n[j + 2] += q.z, n[j + 3] += q.w;
       }
     }
   }
@@ -1003,18 +1094,7 @@ struct Row {
     const bool sharp = !weights || level >= 8 || (level > 1 && shift == 0);
     uint32_t n[kOwn];
     double least[kOwn], most[kOwn], least_sum = 0.0, most_sum = 0.0;
-    static_assert(kOwn % 4 == 0, "bins are read four at a time");
-#pragma unroll
-    for (int j = 0; j < kOwn; ++j) n[j] = 0;
-#pragma unroll 1
-    for (int r = 0; r < blocks; ++r) {
-      const uint32_t *hist = (r ? of((rank + r) & (blocks - 1)) : sh())->hist + threadIdx.x * kOwn;
-#pragma unroll
-      for (int j = 0; j < kOwn; j += 4) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(hist + j);
-        n[j] += q.x, n[j + 1] += q.y, n[j + 2] += q.z, n[j + 3] += q.w;
-      }
-    }
+    bins_of_row(n);
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const uint32_t b = threadIdx.x * kOwn + j;
@@ -1172,7 +1252,7 @@ struct Row {
     const double la = warp_scan(lane < kWarps ? sh()->warp_a[lane & (kWarps - 1)] : 0.0), before = __shfl_sync(0xffffffffu, la, max(warp - 1, 0));
     double run = (warp ? before : 0.0) + (up_to - sum);
     if (from_end) aim += __shfl_sync(0xffffffffu, la, 31);
-    int in_front = 0, unclear = 0;  // of the list, before which less than the aim lies: its front
+    int in_front = 0, unclear = unsure > 0.0 && (n == 0 || !(aim > unsure));  // of the list, before which less than the aim lies: its front
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const int i = threadIdx.x * kOwn + j;
