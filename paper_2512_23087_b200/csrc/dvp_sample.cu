@@ -29,7 +29,7 @@ namespace sample {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kList = 2048;
 constexpr int kTable = 64;
-constexpr int kParts = 128;         // sums that a warp keeps of its part of the row, of one piece or several each
+constexpr int kParts = 64;          // sums that a warp keeps of its part of the row, of one piece or several each
 constexpr int kMostBounds = 32768;  // granules whose maximum is held: 64 KB
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kNoIndex = 0x7fffffff;
@@ -69,6 +69,7 @@ struct Shared {
     uint64_t sorted[kList];
   };
   double part[kWarps][kParts];  // of the last sum over the row; of the first sweep float32 pairs: a maximum, the sum against it
+  float tail[kWarps][kParts];  // of the same parts what lies behind the cut
   double table[kTable];  // 2^(i / kTable)
   double chunk[kWarps];  // the warps' parts of a sum over the row
   double group[32];      // sums of 32 neighbouring logits
@@ -654,7 +655,8 @@ struct Row {
   // have been told: the first that it looks for where it does, or the last of those with something where rounding leaves none.
   // Known to the block that has it alone; the others get -2.  `unsure`: how far the parts may be off; then the answer is
   // kNoIndex where that matters, known to all.
-  __device__ __noinline__ static int find(Row row, const Pass a, double aim, double unsure, bool pairs) {
+  // `pairs`: 0 the parts are sums of the pass, 1 those of the first sweep, 2 those less `tail`.
+  __device__ __noinline__ static int find(Row row, const Pass a, double aim, double unsure, int pairs) {
     const int lane = row.lane, blocks = row.blocks;
     const auto amount = [&](float x, int i) {
       if (!(x >= a.v && x <= a.most && (x > a.v || i <= a.i))) return 0.0;
@@ -690,6 +692,7 @@ struct Row {
           if (pairs && q + lane < parts) {
             const float top = __int_as_float(__double2hiint(part));
             part = top > kNegInf ? (double)__int_as_float(__double2loint(part)) * row.power(((double)top - (double)row.m) * row.inv_t) : 0.0;
+            if (pairs == 2) part = fmax(0.0, part - (double)sh()->tail[of_warp][q + lane]);
           }
           const double end = run + warp_sum(part);
           const int who = passes(part, run);
@@ -751,7 +754,7 @@ struct Row {
     return at;
   }
   // find(), and whether it failed, known to all blocks; `everywhere`: the index too.
-  __device__ __forceinline__ int found(const Pass &a, double aim, double unsure, bool everywhere, bool pairs) {
+  __device__ __forceinline__ int found(const Pass &a, double aim, double unsure, bool everywhere, int pairs) {
     int at = find(*this, a, aim, unsure, pairs);
     if ((everywhere || unsure > 0.0) && blocks > 1) {
       tell(0.0, 0.f, at);
@@ -809,21 +812,23 @@ struct Row {
 
   // Moves the cut to the last logit, in falling order, before which less than share * all lies; weights: sums of weights, else
   // of ones.  Logits below `floor` are known to lie behind it.  `all`: the amount in the whole row, good to `unsure`, of which at
-  // most `below` lies below `floor`.
-  __device__ void select(bool weights, double share, double all, double unsure, float floor, double below) {
+  // most `below` lies below `floor`.  Returns what `chunk` and the parts have then, with `n_kept` the number that is kept: kTail, the
+  // parts less `tail` are the float32 sums of what is kept, good to `kept_unsure`; kExact, its sums in double; kStale.
+  enum Sums { kStale, kTail, kExact };
+  __device__ Sums select(bool weights, double share, double all, double unsure, float floor, double below, double &kept_unsure, int &n_kept) {
     double aim = share * all;
     const float span = floor > 0.5f * kLowest ? m - floor : (float)(40.0 / inv_t);
     const float most = (float)(kBins - 2) / span, per = span > 0.f && most < 1e30f ? most : 0.f;  // 0: all in one bin
     // level 0: bins of distance; from level 1 on logits from `low` to `high`, in bins by their keys
     float low = floor, high = m;
     uint32_t n_in = 0;
-    // A histogram of all that can matter costs more than reading the row again.  Where a warp has pieces enough, one of an eighth
+    // A histogram of all that can matter costs more than reading the row again.  Where a warp has pieces enough, one of a quarter
     // of them guesses where the cut is, and what is found there shows whether it was right.
     bool guess = unsure > 0.0 && all_segs >= 16 * kWarps * blocks;
     if (guess) {
       for (int i = threadIdx.x; i < kBins; i += kThreads) sh()->hist[i] = 0;
       __syncthreads();
-      bins_of_distance(*this, low, per, 0x01010101u << (warp & 7));
+      bins_of_distance(*this, low, per, 0x11111111u << (warp & 3));
       meet();
       window((1.0 - share) * all, below, per);
       n_in = sh()->pick_last;
@@ -849,30 +854,34 @@ struct Row {
       if (threadIdx.x == 0) sh()->list_n = 0;
       __syncthreads();
       Pass a = of_kept(low);
-      a.weights = weights;
+      // weights are summed up in any case: they are wanted next
       a.split = high;  // only the logits above; what is cut already lies at the bracket's end or behind it
       a.rest = ties ? kNone : gather ? kToList : kBinsOfKeys;
       if (ties) a.v = high, a.i = -1;
       a.k_hi = k_hi;
       a.shift = shift;
-      Sum above = {0.0, 0};
+      Sum sums = {0.0, 0};
+      double above = 0.0;
       double tail = 0.0;
+      int n_not = 0;
       if (level == 0) {
         bins_of_distance(*this, low, per, 0xffffffffu);
         meet();
       } else if (gather && unsure > 0.0) {
-        tail = behind(low, high);
+        const Behind b = behind(low, high);
+        tail = b.sum, n_not = b.n_not;
       } else {
-        above = sum(a);
+        sums = sum(a);
+        above = weights ? sums.all : (double)sums.n;
       }
       if (ties) {
         // kept are the first r with above + (r - 1) w < aim
         const double w = weights ? weight(high) : 1.0;
         const auto number = [&](double to) {
-          double r = fmin((double)n_in, fmax(1.0, ceil((to - above.all) / w)));
-          if (r > 1.0 && !(above.all + (r - 1.0) * w < to))
+          double r = fmin((double)n_in, fmax(1.0, ceil((to - above) / w)));
+          if (r > 1.0 && !(above + (r - 1.0) * w < to))
             r -= 1.0;
-          else if (r < (double)n_in && above.all + r * w < to)
+          else if (r < (double)n_in && above + r * w < to)
             r += 1.0;
           return r;
         };
@@ -881,9 +890,9 @@ struct Row {
         a.most = high;
         a.weights = false;
         sum(a);
-        cut_i = found(a, r - 0.5, 0.0, true, false);
+        cut_i = found(a, r - 0.5, 0.0, true, 0);
         cut_v = high;
-        return;
+        return kStale;
       }
       if (gather) {
         // all blocks' lists in one, alike in every block
@@ -903,41 +912,71 @@ struct Row {
         }
         if (n <= kList) sort_list(n);
         int last;
-        if (guess) {
-          const double end = (1.0 - share) * all;
-          if (n > kList || !cut_from_list(true, n, tail - end, true, (1.0 - share) * unsure + tail * eps(tail), last)) {
+        Sums have = kExact;
+        if (unsure > 0.0) {
+          // Kept is what has more than (1 - share) all at and behind it.  Of that side's sums, the whole's and the tail's, float32's
+          // errors are the smaller by 1 - share; mostly nothing lies so near the border that they matter.
+          const Border at = n <= kList ? cut_from_list(true, n, tail - (1.0 - share) * all, true, (1.0 - share) * unsure + tail * eps(tail), last)
+                                       : kOutside;
+          if (at == kOutside && guess) {
             guess = false;  // the long way then
             low = floor, high = m;
             level = -1;
             continue;
           }
-        } else if (unsure > 0.0) {
-          // Kept is what has more than (1 - share) all at and behind it.  Of that side's sums, the whole's and the tail's, float32's
-          // errors are the smaller by 1 - share; mostly nothing lies so near the border that they matter.
-          const double end = (1.0 - share) * all;
-          if (!cut_from_list(true, n, tail - end, true, (1.0 - share) * unsure + tail * eps(tail), last)) {
+          have = kTail;
+          if (at != kClear) {
             for (int i = threadIdx.x; i < n; i += kThreads) sh()->list[i] = sh()->sorted[i];  // passes take their place
             __syncthreads();
             aim = share * whole();
             a.v = high;
             a.i = -1;
             a.rest = kNone;
-            above = sum(a);
+            sums = sum(a);
             for (int i = threadIdx.x; i < n; i += kThreads) sh()->sorted[i] = sh()->list[i];
             __syncthreads();
-            cut_from_list(true, n, aim - above.all, false, 0.0, last);
+            cut_from_list(true, n, aim - sums.all, false, 0.0, last);
+            have = kExact;
           }
         } else {
-          cut_from_list(weights, n, aim - above.all, false, 0.0, last);
+          cut_from_list(weights, n, aim - above, false, 0.0, last);
         }
         set_cut(last);
-        return;
+        {
+          // The list's logits: those behind the cut go to the tail, or the kept ones to the exact sums, of the warp that has their
+          // pieces and of their part.
+          const int each = (segs + kWarps - 1) / kWarps;
+          const int lo_i = (seg0 + warp * each) * 32 * kPer - off, hi_i = (seg0 + min(segs, (warp + 1) * each)) * 32 * kPer - off;
+          const int from = have == kTail ? last + 1 : 0, to = have == kTail ? n : last + 1;
+          double acc = 0.0;
+#pragma unroll 1
+          for (int i = from + lane; i < to; i += 32) {
+            const uint64_t item = sh()->sorted[i];
+            const int at = (int)(uint32_t)item;
+            if (at >= lo_i && at < hi_i) {
+              const double w = weight(value_of(~(uint32_t)(item >> 32)));
+              const int part = ((at - lo_i) / (32 * kPer)) >> log_q;
+              acc += w;
+              // in any order: the parts say where to look, and their roundings are of the size of all others
+              if (have == kTail)
+                atomicAdd(&sh()->tail[warp][part], (float)w);
+              else
+                atomicAdd(&sh()->part[warp][part], w);
+            }
+          }
+          acc = warp_sum(acc);
+          if (lane == 0) sh()->chunk[warp] += have == kTail ? -(sh()->warp_b[warp] + acc) : acc;
+          n_kept = have == kTail ? n_not - (n - 1 - last) : sums.n + last + 1;
+          kept_unsure = unsure + tail * eps(tail);
+          __syncthreads();
+        }
+        return have;
       }
-      bracket(weights, level, aim, above.all, all, share * unsure, below, unsure, per, k_lo, k_hi, shift);
+      bracket(weights, level, aim, above, all, share * unsure, below, unsure, per, k_lo, k_hi, shift);
       const uint32_t lo = sh()->pick_lo, hi = sh()->pick_hi;
       n_in = sh()->pick_last;
       meet();  // the histograms have been read
-      if (n_in == 0) return;  // less than the aim in all: everything stays
+      if (n_in == 0) return kStale;  // less than the aim in all: everything stays
       if (level == 0) {
         edges(lo, hi, per, low, high);
       } else {
@@ -945,6 +984,7 @@ struct Row {
         high = value_of(k_hi - (lo << shift));
       }
     }
+    return kStale;
   }
   // The values, from low to high, that the logits in bins lo to hi can have; 2^-20 covers the roundings of the distance.
   __device__ __forceinline__ void edges(uint32_t lo, uint32_t hi, float per, float &low, float &high) const {
@@ -953,8 +993,8 @@ struct Row {
     high = fminf(m, __double2float_ru((double)m - (double)lo / per * (1.0 - slack)));
     if (hi < kBins - 1) low = fmaxf(low, __double2float_rd((double)m - ((double)hi + 1.0) / per * (1.0 + slack)));
   }
-  // From the histograms of an eighth of the row: the bins in which the sum over what lies behind can fall below `end`, within four
-  // standard deviations and 2 %: pick_lo to pick_hi, which may have pick_last logits.  Every block alike.
+  // From the histograms of a quarter of the row: the bins in which the sum over what lies behind can fall below `end`, within three
+  // standard deviations and 0.5 %: pick_lo to pick_hi, which may have pick_last logits.  Every block alike.
   __device__ void window(double end, double below, float per) {
     constexpr int kOwn = kBins / kThreads;
     uint32_t n[kOwn];
@@ -984,9 +1024,9 @@ struct Row {
     for (int j = 0; j < kOwn; ++j) {
       behind_w -= (float)n[j] * w[j];
       behind_s -= (float)n[j] * w[j] * w[j];
-      const float off = 4.f * sqrtf(56.f * fmaxf(behind_s, 0.f)) + 0.02f * (float)end + (float)below;
-      if (8.f * behind_w - off < (float)end) lo = min(lo, threadIdx.x * kOwn + j);
-      if (8.f * behind_w + off < (float)end) hi = min(hi, threadIdx.x * kOwn + j);
+      const float off = 3.f * sqrtf(12.f * fmaxf(behind_s, 0.f)) + 0.005f * (float)end + (float)below;
+      if (4.f * behind_w - off < (float)end) lo = min(lo, threadIdx.x * kOwn + j);
+      if (4.f * behind_w + off < (float)end) hi = min(hi, threadIdx.x * kOwn + j);
     }
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_min_sync(0xffffffffu, hi);
@@ -1005,7 +1045,7 @@ struct Row {
     inside = __reduce_add_sync(0xffffffffu, inside);
     if (threadIdx.x == 0) sh()->pick_last = 0;
     __syncthreads();
-    if (lane == 0 && inside) atomicAdd(&sh()->pick_last, 8 * inside);
+    if (lane == 0 && inside) atomicAdd(&sh()->pick_last, 4 * inside);
     __syncthreads();
   }
   // The row's numbers in the thread's bins.
@@ -1035,9 +1075,17 @@ struct Row {
   }
   // Of a row that nothing is cut from: the float32 sum of the weights of logits below `low`, with what lies from there to `high` to
   // the list.  Leaves `chunk` alone.
-  __device__ __noinline__ static double behind_of_warp(const Row row, float low, float high) { return row.sweep_behind(low, high); }
-  __device__ __forceinline__ double sweep_behind(float low, float high) const {
+  struct Behind {
+    double sum;
+    int n_not;  // logits that are not behind
+  };
+  __device__ __noinline__ static Behind behind_of_warp(const Row row, float low, float high) { return row.sweep_behind(low, high); }
+  __device__ __forceinline__ Behind sweep_behind(float low, float high) const {
     double s = 0.0;
+    int n_not = 0;
+    float *tails = sh()->tail[warp];
+    for (int q = lane; q < kParts; q += 32) tails[q] = 0.f;
+    __syncwarp();
     uint32_t next[8];
     if (mine > 0) load(first, next);
 #pragma unroll 1
@@ -1047,15 +1095,22 @@ struct Row {
       for (int j = 0; j < 8; ++j) w[j] = next[j];
       if (i + 1 < mine) load(first + i + 1, next);
       const int i0 = first_of(first + i);
-      unsigned out = 0, in = 0;  // not in the sum; in the list
+      unsigned out = 0, from_low = 0, to_high = 0;
 #pragma unroll
       for (int j = 0; j < kPer / 2; ++j) {
         float a, b;
         two_of<T>(w, j, a, b);
-        out |= (a < low && !((a - m) * c < -1e4f) ? 0u : 1u) << (2 * j) | (b < low && !((b - m) * c < -1e4f) ? 0u : 1u) << (2 * j + 1);
-        in |= (a >= low && a <= high ? 1u : 0u) << (2 * j) | (b >= low && b <= high ? 1u : 0u) << (2 * j + 1);
+        from_low |= (a >= low ? 1u : 0u) << (2 * j) | (b >= low ? 1u : 0u) << (2 * j + 1);
+        to_high |= (a <= high ? 1u : 0u) << (2 * j) | (b <= high ? 1u : 0u) << (2 * j + 1);
+        out |= ((a - m) * c < -1e4f ? 1u : 0u) << (2 * j) | ((b - m) * c < -1e4f ? 1u : 0u) << (2 * j + 1);
       }
-      s += (double)terms<true>(w, m, out);
+      const unsigned in = from_low & to_high;
+      n_not += __popc(from_low);
+      const float g = warp_sum(terms<true>(w, m, out | from_low));
+      if (lane == 0) {
+        tails[i >> log_q] += g;
+        s += (double)g;
+      }
       if (!__any_sync(0xffffffffu, in != 0)) continue;
 #pragma unroll
       for (int j = 0; j < kPer / 2; ++j) {
@@ -1065,19 +1120,27 @@ struct Row {
         if (in >> (2 * j + 1) & 1) to_list(b, i0 + 2 * j + 1);
       }
     }
-    return warp_sum(s);
+    return Behind{__shfl_sync(0xffffffffu, s, 0), (int)__reduce_add_sync(0xffffffffu, n_not)};
   }
-  __device__ double behind(float low, float high) {
-    const double ws = behind_of_warp(*this, low, high);
+  // The warps' sums stay in warp_b.
+  __device__ Behind behind(float low, float high) {
+    const Behind w = behind_of_warp(*this, low, high);
     __syncthreads();
-    if (lane == 0) sh()->warp_a[warp] = ws;
-    __syncthreads();
-    double own = warp_sum(lane < kWarps ? sh()->warp_a[lane & (kWarps - 1)] : 0.0);
-    if (blocks > 1) {
-      tell(own, 0.f, 0);
-      own = warp_sum(lane < blocks ? told(lane & (blocks - 1)).a : 0.0);
+    if (lane == 0) {
+      sh()->warp_b[warp] = w.sum;
+      sh()->warp_n[warp] = (uint32_t)w.n_not;
     }
-    return own;
+    __syncthreads();
+    Behind r;
+    r.sum = warp_sum(lane < kWarps ? sh()->warp_b[lane & (kWarps - 1)] : 0.0);
+    r.n_not = (int)__reduce_add_sync(0xffffffffu, lane < kWarps ? sh()->warp_n[lane & (kWarps - 1)] : 0u);
+    if (blocks > 1) {
+      tell(r.sum, 0.f, r.n_not);
+      const Slot o = told(lane & (blocks - 1));
+      r.sum = warp_sum(lane < blocks ? o.a : 0.0);
+      r.n_not = (int)__reduce_add_sync(0xffffffffu, lane < blocks ? o.i : 0);
+    }
+    return r;
   }
   // The least key of bin b, of keys from k_lo to k_hi: bin 0 has the largest.
   __device__ __forceinline__ static uint32_t edge_of(uint32_t k_lo, uint32_t k_hi, uint32_t b, int shift) {
@@ -1236,7 +1299,8 @@ struct Row {
   }
   // The last of the sorted list before which less than the aim lies; returns whether that is so for every aim within `unsure`.
   // `from_end`: the aim is against the list's sum.
-  __device__ bool cut_from_list(bool weights, int n, double aim, bool from_end, double unsure, int &last) {
+  enum Border { kClear, kNear, kOutside };
+  __device__ Border cut_from_list(bool weights, int n, double aim, bool from_end, double unsure, int &last) {
     constexpr int kOwn = kList / kThreads;
     double w[kOwn], sum = 0.0;
 #pragma unroll
@@ -1252,22 +1316,23 @@ struct Row {
     const double la = warp_scan(lane < kWarps ? sh()->warp_a[lane & (kWarps - 1)] : 0.0), before = __shfl_sync(0xffffffffu, la, max(warp - 1, 0));
     double run = (warp ? before : 0.0) + (up_to - sum);
     if (from_end) aim += __shfl_sync(0xffffffffu, la, 31);
-    int in_front = 0, unclear = unsure > 0.0 && (n == 0 || !(aim > unsure));  // of the list, before which less than the aim lies: its front
+    int in_front = 0, near = 0, outside = unsure > 0.0 && (n == 0 || !(aim > unsure));  // of the list, before which less than the aim lies: its front
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const int i = threadIdx.x * kOwn + j;
       in_front += i < n && (run < aim || i == 0);
-      // the bracket holds the cut: its first logit is kept, and its end is behind the aim
-      unclear |= unsure > 0.0 && i < n && i > 0 && fabs(run - aim) <= unsure;
+      // the list holds the cut where its first logit is kept, and its end is behind the aim
+      near |= unsure > 0.0 && i < n && i > 0 && fabs(run - aim) <= unsure;
       run += w[j];
-      unclear |= unsure > 0.0 && i == n - 1 && run - aim <= unsure;
+      outside |= unsure > 0.0 && i == n - 1 && run - aim <= unsure;
     }
     in_front = __reduce_add_sync(0xffffffffu, in_front);
     if (lane == 0) sh()->warp_n[warp] = (uint32_t)in_front;
-    unclear = __syncthreads_or(unclear);
+    near = __syncthreads_or(near);
+    outside = __syncthreads_or(outside);
     last = (int)__reduce_add_sync(0xffffffffu, lane < kWarps ? sh()->warp_n[lane & (kWarps - 1)] : 0u) - 1;
     __syncthreads();  // warp_n and warp_a have been read
-    return !unclear;
+    return outside ? kOutside : near ? kNear : kClear;
   }
 };
 
@@ -1329,6 +1394,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
       count = 1;
     } else {
       bool whole = row.cut_v == kLowest;  // nothing is cut: the sums of the first sweep are those of what is kept
+      typename Row<T>::Sums have = Row<T>::kStale;
+      double kept_unsure = 0.0;
 #pragma unroll 1
       for (int step = 0; step < 2; ++step) {  // top_k, then top_p
         const bool weights = step == 1;
@@ -1349,7 +1416,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
         } else {
           floor = row.floor_of(top_k);
         }
-        row.select(weights, share, all, unsure, floor, below);
+        have = row.select(weights, share, all, unsure, floor, below, kept_unsure, count);
         whole = false;
       }
       // by the warps' float32 sums where nothing is cut, unless the border is too near for them
@@ -1359,16 +1426,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
 #pragma unroll 1
       while (id == kNoIndex) {
         double unsure = 0.0;
-        if (whole) {
+        if (whole || have != Row<T>::kStale) {
           all = row.sum_of_chunks();
-          unsure = 2.0 * row.eps(all) * all;
-          count = (int)p.V - masked;
+          unsure = have == Row<T>::kExact ? 0.0 : 2.0 * (whole ? row.eps(all) * all : kept_unsure);
+          if (whole) count = (int)p.V - masked;
+          // a logarithm near zero wants all of its sum's digits
+          if (have == Row<T>::kTail && !(all > 1.5)) {
+            have = Row<T>::kStale;
+            continue;
+          }
         } else {
           const typename Row<T>::Sum r = row.sum(row.of_kept(kLowest));
           all = r.all;
           count = r.n;
         }
-        id = row.found(row.of_kept(kLowest), (double)u * all, unsure, false, whole);
+        id = row.found(row.of_kept(kLowest), (double)u * all, unsure, false, whole ? 1 : have == Row<T>::kTail ? 2 : 0);
+        if (id == kNoIndex) have = Row<T>::kStale;
         whole = false;
       }
       kept_rest = was_whole ? rest : all - 1.0;
