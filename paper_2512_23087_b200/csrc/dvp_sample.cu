@@ -32,6 +32,7 @@ constexpr int kTable = 64;
 constexpr int kParts = 64;          // sums that a warp keeps of its part of the row, of one piece or several each
 constexpr int kMostBounds = 32768;  // granules whose maximum is held: 64 KB
 constexpr float kLowest = -3.402823466e38f;
+constexpr double kRound = 5.9604644775390625e-08;  // 2^-24, half a step of float32
 constexpr int kNoIndex = 0x7fffffff;
 constexpr long long kMostRows = 0x0fffffffLL, kMostLogits = 0x7fff0000LL;
 
@@ -69,7 +70,7 @@ struct Shared {
     uint64_t sorted[kList];
   };
   double part[kWarps][kParts];  // of the last sum over the row; of the first sweep float32 pairs: a maximum, the sum against it
-  float tail[kWarps][kParts];  // of the same parts what lies behind the cut
+  double tail[kWarps][kParts];  // of the same parts what lies behind the cut
   double table[kTable];  // 2^(i / kTable)
   double chunk[kWarps];  // the warps' parts of a sum over the row
   double group[32];      // sums of 32 neighbouring logits
@@ -424,12 +425,13 @@ struct Row {
     apart(add2(sum[0], sum[1]), lo, hi);
     return lo + hi;
   }
-  // How far a sum S of terms() can be off, relative to itself.  With p_k a logit's share of S, its exponent is -log2 p_k - log2 S, and
-  // the mean of these at most the entropy, log2 V, less log2 S.  A difference is rounded once: ln 2 times that mean, times
-  // 2^-24; the exponential is good to 4, what is left of product and c to 1, and a granule's additions take 8 at most.
-  __device__ __forceinline__ double eps(double sum) const {
+  // How far a sum S of terms(), of the row or any of its logits, can be off.  With p_k a logit's share of S, its exponent is
+  // -log2 p_k - log2 S, and the mean of these at most the entropy, log2 V, less log2 S.  A difference is rounded once: ln 2 times that
+  // mean, times 2^-24; the exponential is good to 4, what is left of product and c to 1, and a granule's additions take 5 at most.
+  // It grows with S.
+  __device__ __forceinline__ double error(double sum) const {
     const int bits = 32 - __clz(V) + max(0, 1023 - (int)(__double2hiint(sum) >> 20 & 0x7ff));
-    return (13.0 + 0.6932 * (double)bits) * 5.9604644775390625e-08;
+    return (11.0 + 0.6932 * (double)bits) * kRound * sum;
   }
 
   // A bit for each of a granule's logits that is at least v; those of 16 bits are compared two at a time, with the least value of
@@ -451,6 +453,50 @@ struct Row {
       mask = (mask | mask >> 16) & 0xffff;
     }
     return mask;
+  }
+
+  // The same for logits above v, with the largest value of the type that is not above it.
+  __device__ __forceinline__ static unsigned over(const uint32_t (&w)[8], float v) {
+    unsigned mask = 0;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) mask |= __uint_as_float(w[j]) > v ? 1u << j : 0u;
+    } else {
+      using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+      T2 most;
+      if constexpr (std::is_same<T, __half>::value)
+        most.x = most.y = __float2half_rd(v);
+      else
+        most.x = most.y = __float2bfloat16_rd(v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mask |= __hgt2_mask(reinterpret_cast<const T2 &>(w[i]), most) & (1u << (2 * i) | 1u << (17 + 2 * i));
+      mask = (mask | mask >> 16) & 0xffff;
+    }
+    return mask;
+  }
+  // A granule with `far` in the place of logits of at least v and below itself.
+  __device__ __forceinline__ static void clamp(const uint32_t (&w)[8], float v, T far, uint32_t (&to)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const float x = __uint_as_float(w[j]);
+        to[j] = __float_as_uint(x >= v ? far : fmaxf(x, far));
+      }
+    } else {
+      using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+      T2 least, lowest;
+      if constexpr (std::is_same<T, __half>::value)
+        least.x = least.y = __float2half_ru(v);
+      else
+        least.x = least.y = __float2bfloat16_ru(v);
+      lowest.x = lowest.y = far;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const T2 x = reinterpret_cast<const T2 &>(w[i]), raised = __hmax2(x, lowest);
+        const uint32_t mask = __hge2_mask(x, least);
+        to[i] = (reinterpret_cast<const uint32_t &>(lowest) & mask) | (reinterpret_cast<const uint32_t &>(raised) & ~mask);
+      }
+    }
   }
 
   // Of the warp's pieces i0 to i0 + 31 those with a granule that reaches `v`: a bit each.
@@ -497,6 +543,8 @@ struct Row {
     uint32_t k_hi;   // kBinsOfKeys
     int shift;
   };
+  // What `chunk` and the parts have of what is kept: see select().
+  enum Sums { kStale, kTail, kExact };
   // What is kept, none below `from`.
   __device__ __forceinline__ Pass of_kept(float from) const {
     return Pass{fmaxf(from, cut_v), from > cut_v ? kNoIndex : cut_i, -kNegInf, kNegInf, true, kNone, 0, 0};
@@ -533,7 +581,17 @@ struct Row {
       const int own = __popc(mask), up_to = warp_scan(own), all = __shfl_sync(0xffffffffu, up_to, 31);
       double of_piece = 0.0;
       int at = up_to - own;
-      if (a.rest == kNone) {
+      if (a.rest == kNone && a.weights && all >= 16 * kPer) {
+        // most of them: as they lie
+#pragma unroll
+        for (int j = 0; j < kPer / 2; ++j) {
+          float lo, hi;
+          two_of<T>(w, j, lo, hi);
+          const double one = row.weight(lo), two = row.weight(hi);
+          of_piece += (mask >> (2 * j) & 1 ? one : 0.0) + (mask >> (2 * j + 1) & 1 ? two : 0.0);
+        }
+        n += own;
+      } else if (a.rest == kNone) {
         // sums alone: two side by side, as one exponential is a long chain
 #pragma unroll
         for (int j = 0; j < kPer / 2; ++j) {
@@ -655,8 +713,9 @@ struct Row {
   // have been told: the first that it looks for where it does, or the last of those with something where rounding leaves none.
   // Known to the block that has it alone; the others get -2.  `unsure`: how far the parts may be off; then the answer is
   // kNoIndex where that matters, known to all.
-  // `pairs`: 0 the parts are sums of the pass, 1 those of the first sweep, 2 those less `tail`.
-  __device__ __noinline__ static int find(Row row, const Pass a, double aim, double unsure, int pairs) {
+  // `have`: the parts are sums of the pass (kExact), or those of the first sweep, of which `behind` is known to lie behind the cut
+  // (kTail): their own roundings come to `unsure` then.
+  __device__ __noinline__ static int find(Row row, const Pass a, double aim, double unsure, Sums have, double behind) {
     const int lane = row.lane, blocks = row.blocks;
     const auto amount = [&](float x, int i) {
       if (!(x >= a.v && x <= a.most && (x > a.v || i <= a.i))) return 0.0;
@@ -679,6 +738,8 @@ struct Row {
     if (owner == row.rank) {
       // the warp whose part it is
       const int of_warp = max(0, passes(lane < kWarps ? sh()->chunk[lane & (kWarps - 1)] : 0.0, run));
+      // a lane's float32 sum has two additions and a product by a rounded factor a piece, and five additions join the lanes
+      if (have == kTail) unsure += (double)(6 + (4 << row.log_q)) * kRound * (sh()->chunk[of_warp] + 2.0 * behind);
       const int per = (row.segs + kWarps - 1) / kWarps, s0 = of_warp * per, s1 = min(row.segs, s0 + per);
       // its parts, every warp alike
       int part_of = 0, piece = -1;
@@ -689,10 +750,10 @@ struct Row {
 #pragma unroll 1
         for (int q = 0; q < parts && piece < 0; q += 32) {
           double part = q + lane < parts ? stored[q + lane] : 0.0;
-          if (pairs && q + lane < parts) {
+          if (have == kTail && q + lane < parts) {
             const float top = __int_as_float(__double2hiint(part));
             part = top > kNegInf ? (double)__int_as_float(__double2loint(part)) * row.power(((double)top - (double)row.m) * row.inv_t) : 0.0;
-            if (pairs == 2) part = fmax(0.0, part - (double)sh()->tail[of_warp][q + lane]);
+            if (behind > 0.0) part = fmax(0.0, part - sh()->tail[of_warp][q + lane]);
           }
           const double end = run + warp_sum(part);
           const int who = passes(part, run);
@@ -754,8 +815,8 @@ struct Row {
     return at;
   }
   // find(), and whether it failed, known to all blocks; `everywhere`: the index too.
-  __device__ __forceinline__ int found(const Pass &a, double aim, double unsure, bool everywhere, int pairs) {
-    int at = find(*this, a, aim, unsure, pairs);
+  __device__ __forceinline__ int found(const Pass &a, double aim, double unsure, bool everywhere, Sums have, double behind) {
+    int at = find(*this, a, aim, unsure, have, behind);
     if ((everywhere || unsure > 0.0) && blocks > 1) {
       tell(0.0, 0.f, at);
       const int any = __reduce_max_sync(0xffffffffu, told(lane & (blocks - 1)).i);
@@ -813,9 +874,8 @@ struct Row {
   // Moves the cut to the last logit, in falling order, before which less than share * all lies; weights: sums of weights, else
   // of ones.  Logits below `floor` are known to lie behind it.  `all`: the amount in the whole row, good to `unsure`, of which at
   // most `below` lies below `floor`.  Returns what `chunk` and the parts have then, with `n_kept` the number that is kept: kTail, the
-  // parts less `tail` are the float32 sums of what is kept, good to `kept_unsure`; kExact, its sums in double; kStale.
-  enum Sums { kStale, kTail, kExact };
-  __device__ Sums select(bool weights, double share, double all, double unsure, float floor, double below, double &kept_unsure, int &n_kept) {
+  // first sweep's parts and `tail` of them what is not kept; kExact, sums of what is kept in double; kStale.
+  __device__ Sums select(bool weights, double share, double all, double unsure, float floor, double below, int &n_kept) {
     double aim = share * all;
     const float span = floor > 0.5f * kLowest ? m - floor : (float)(40.0 / inv_t);
     const float most = (float)(kBins - 2) / span, per = span > 0.f && most < 1e30f ? most : 0.f;  // 0: all in one bin
@@ -890,7 +950,7 @@ struct Row {
         a.most = high;
         a.weights = false;
         sum(a);
-        cut_i = found(a, r - 0.5, 0.0, true, 0);
+        cut_i = found(a, r - 0.5, 0.0, true, kExact, 0.0);
         cut_v = high;
         return kStale;
       }
@@ -910,13 +970,13 @@ struct Row {
           n_in = (uint32_t)n;
           continue;
         }
-        if (n <= kList) sort_list(n);
+        if (n <= kList) sort_list(n, k_lo, k_hi);
         int last;
         Sums have = kExact;
         if (unsure > 0.0) {
           // Kept is what has more than (1 - share) all at and behind it.  Of that side's sums, the whole's and the tail's, float32's
           // errors are the smaller by 1 - share; mostly nothing lies so near the border that they matter.
-          const Border at = n <= kList ? cut_from_list(true, n, tail - (1.0 - share) * all, true, (1.0 - share) * unsure + tail * eps(tail), last)
+          const Border at = n <= kList ? cut_from_list(true, n, tail - (1.0 - share) * all, true, (1.0 - share) * unsure + error(tail), last)
                                        : kOutside;
           if (at == kOutside && guess) {
             guess = false;  // the long way then
@@ -945,29 +1005,36 @@ struct Row {
         {
           // The list's logits: those behind the cut go to the tail, or the kept ones to the exact sums, of the warp that has their
           // pieces and of their part.
+          // Whole numbers of 2^-52 of the largest are added, in any order.
+          static_assert(kBins * sizeof(uint32_t) == kWarps * kParts * sizeof(uint64_t), "the sums lie in the histogram");
+          unsigned long long *sums_of = reinterpret_cast<unsigned long long *>(sh()->hist);
           const int each = (segs + kWarps - 1) / kWarps;
-          const int lo_i = (seg0 + warp * each) * 32 * kPer - off, hi_i = (seg0 + min(segs, (warp + 1) * each)) * 32 * kPer - off;
           const int from = have == kTail ? last + 1 : 0, to = have == kTail ? n : last + 1;
-          double acc = 0.0;
-#pragma unroll 1
-          for (int i = from + lane; i < to; i += 32) {
+          for (int i = threadIdx.x; i < kWarps * kParts; i += kThreads) sums_of[i] = 0;
+          __syncthreads();
+          const double largest = from < to ? weight(value_of(~(uint32_t)(sh()->sorted[from] >> 32))) : 1.0;
+          const double up = 4503599627370496.0 / fmax(largest, 1e-290);
+          for (int i = from + threadIdx.x; i < to; i += kThreads) {
             const uint64_t item = sh()->sorted[i];
-            const int at = (int)(uint32_t)item;
-            if (at >= lo_i && at < hi_i) {
-              const double w = weight(value_of(~(uint32_t)(item >> 32)));
-              const int part = ((at - lo_i) / (32 * kPer)) >> log_q;
-              acc += w;
-              // in any order: the parts say where to look, and their roundings are of the size of all others
-              if (have == kTail)
-                atomicAdd(&sh()->tail[warp][part], (float)w);
-              else
-                atomicAdd(&sh()->part[warp][part], w);
-            }
+            const int piece = (int)((uint32_t)item + off) / (32 * kPer) - seg0;
+            if (piece < 0 || piece >= segs) continue;
+            const int of = piece / each;
+            atomicAdd(&sums_of[of * kParts + ((piece - of * each) >> log_q)],
+                      (unsigned long long)__double2ll_rn(weight(value_of(~(uint32_t)(item >> 32))) * up));
+          }
+          __syncthreads();
+          double acc = 0.0;
+          for (int q = lane; q < kParts; q += 32) {
+            const double v = (double)sums_of[warp * kParts + q] * (fmax(largest, 1e-290) * 2.220446049250313e-16);
+            acc += v;
+            if (have == kTail)
+              sh()->tail[warp][q] += v;
+            else
+              sh()->part[warp][q] += v;
           }
           acc = warp_sum(acc);
           if (lane == 0) sh()->chunk[warp] += have == kTail ? -(sh()->warp_b[warp] + acc) : acc;
           n_kept = have == kTail ? n_not - (n - 1 - last) : sums.n + last + 1;
-          kept_unsure = unsure + tail * eps(tail);
           __syncthreads();
         }
         return have;
@@ -1083,43 +1150,74 @@ struct Row {
   __device__ __forceinline__ Behind sweep_behind(float low, float high) const {
     double s = 0.0;
     int n_not = 0;
-    float *tails = sh()->tail[warp];
-    for (int q = lane; q < kParts; q += 32) tails[q] = 0.f;
+    double *tails = sh()->tail[warp];
+    for (int q = lane; q < kParts; q += 32) tails[q] = 0.0;
     __syncwarp();
-    uint32_t next[8];
-    if (mine > 0) load(first, next);
+    // a logit without weight, which takes the place of what is not behind and of all that lies below it
+    const T far = Storage<T>::narrow(m - 1000.f / c);
+    const float at_far = (Storage<T>::widen(far) - m) * c;
+    const bool clamped = at_far < -200.f && at_far > -5000.f;
+    // granules with something for the list: few, so they wait until a warp's lanes can take one each
+    constexpr int kMost = Shared::kPiece;
+    uint32_t *granule = reinterpret_cast<uint32_t *>(sh()->compact.value[warp]);
+    uint16_t *which = sh()->compact.place[warp];
+    int waiting = 0;
+    const auto drain = [&] {
+      __syncwarp();
+#pragma unroll 1
+      for (int e = lane; e < waiting; e += 32) {
+        const int i0 = (int)((seg0 + first) * 32 + granule[e]) * kPer - off;
+#pragma unroll 1
+        for (unsigned mask = which[e]; mask; mask &= mask - 1) {
+          const int i = i0 + __ffs(mask) - 1;
+          to_list(Storage<T>::widen(z[i]), i);
+        }
+      }
+      __syncwarp();
+      waiting = 0;
+    };
+    uint32_t next[2][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (u < mine) load(first + u, next[u]);
 #pragma unroll 1
     for (int i = 0; i < mine; ++i) {
       uint32_t w[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = next[j];
-      if (i + 1 < mine) load(first + i + 1, next);
-      const int i0 = first_of(first + i);
-      unsigned out = 0, from_low = 0, to_high = 0;
-#pragma unroll
-      for (int j = 0; j < kPer / 2; ++j) {
-        float a, b;
-        two_of<T>(w, j, a, b);
-        from_low |= (a >= low ? 1u : 0u) << (2 * j) | (b >= low ? 1u : 0u) << (2 * j + 1);
-        to_high |= (a <= high ? 1u : 0u) << (2 * j) | (b <= high ? 1u : 0u) << (2 * j + 1);
-        out |= ((a - m) * c < -1e4f ? 1u : 0u) << (2 * j) | ((b - m) * c < -1e4f ? 1u : 0u) << (2 * j + 1);
-      }
-      const unsigned in = from_low & to_high;
+      for (int j = 0; j < 8; ++j) w[j] = next[0][j], next[0][j] = next[1][j];
+      if (i + 2 < mine) load(first + i + 2, next[1]);
+      const unsigned from_low = from(w, low), in = from_low & ~over(w, high);
       n_not += __popc(from_low);
-      const float g = warp_sum(terms<true>(w, m, out | from_low));
+      float g;
+      if (clamped) {
+        uint32_t v[8];
+        clamp(w, low, far, v);
+        g = terms<false>(v, m, 0);
+      } else {
+        unsigned out = 0;
+#pragma unroll
+        for (int j = 0; j < kPer / 2; ++j) {
+          float a, b;
+          two_of<T>(w, j, a, b);
+          out |= ((a - m) * c < -1e4f ? 1u : 0u) << (2 * j) | ((b - m) * c < -1e4f ? 1u : 0u) << (2 * j + 1);
+        }
+        g = terms<true>(w, m, out | from_low);
+      }
+      g = warp_sum(g);
       if (lane == 0) {
-        tails[i >> log_q] += g;
+        tails[i >> log_q] += (double)g;
         s += (double)g;
       }
-      if (!__any_sync(0xffffffffu, in != 0)) continue;
-#pragma unroll
-      for (int j = 0; j < kPer / 2; ++j) {
-        float a, b;
-        two_of<T>(w, j, a, b);
-        if (in >> (2 * j) & 1) to_list(a, i0 + 2 * j);
-        if (in >> (2 * j + 1) & 1) to_list(b, i0 + 2 * j + 1);
+      const unsigned some = __ballot_sync(0xffffffffu, in != 0);
+      if (in != 0) {
+        const int at = waiting + __popc(some & ((1u << lane) - 1u));
+        granule[at] = (uint32_t)(i * 32 + lane);
+        which[at] = (uint16_t)in;
       }
+      waiting += __popc(some);
+      if (waiting > kMost - 32) drain();
     }
+    drain();
     return Behind{__shfl_sync(0xffffffffu, s, 0), (int)__reduce_add_sync(0xffffffffu, n_not)};
   }
   // The warps' sums stay in warp_b.
@@ -1246,59 +1344,86 @@ struct Row {
     __syncthreads();
   }
 
-  // Sorts the n items of `sorted`: falling logits, rising indices.
-  __device__ void sort_list(int n) {
+  // Sorts the n items of `sorted`, logits of keys from k_lo to k_hi: falling logits, rising indices.  Where a logit's place among
+  // those keys and its index fit 32 bits, which they do for most lists of 16-bit logits, these are sorted: half of the shuffles, and
+  // a comparison is one instruction (some 1,700 logits of 1,024 rows of 151,936: 709 us a call with 64 bits).
+  __device__ void sort_list(int n, uint32_t k_lo, uint32_t k_hi) {
     __syncthreads();
-    if (n <= kThreads) {
-      // an item a thread; partners in the same warp are met by shuffles
-      const int i = threadIdx.x;
-      uint64_t x = i < n ? sh()->sorted[i] : ~0ull;
-      int size = 32;
-      while (size < n) size <<= 1;
-      const bool in = (i & ~31) < size;
-#pragma unroll 1
-      for (int k = 2; k <= size; k <<= 1)
-#pragma unroll 1
-        for (int j = k >> 1; j > 0; j >>= 1) {
-          uint64_t y;
-          if (j >= 32) {
-            __syncthreads();
-            if (in) sh()->sorted[i] = x;
-            __syncthreads();
-            y = in ? sh()->sorted[i ^ j] : x;
-          } else {
-            y = __shfl_xor_sync(0xffffffffu, x, j);
-          }
-          const bool low = (i & j) == 0, rising = (i & k) == 0;
-          if ((low == rising) ? y < x : y > x) x = y;
-        }
-      __syncthreads();
-      if (in) sh()->sorted[i] = x;
-      __syncthreads();
-      return;
+    constexpr int kLow = sizeof(T) == 4 ? 0 : std::is_same<T, __half>::value ? 13 : 16;  // of a key: all 0 or, below zero, all 1
+    const int of_index = 32 - __clz(V), of_key = 32 - __clz((k_hi >> kLow) - (k_lo >> kLow));
+    if (of_index + of_key <= 32) {
+      sort_items<uint32_t>(n, [&](uint64_t item) {
+        return of_key ? ((k_hi >> kLow) - (~(uint32_t)(item >> 32) >> kLow)) << of_index | (uint32_t)item : (uint32_t)item;
+      }, [&](uint32_t x) {
+        uint32_t key = (k_hi >> kLow) - (of_key ? x >> of_index : 0u);
+        key = key << kLow | (key >> (31 - kLow) & 1 ? 0u : (1u << kLow) - 1u);
+        return (uint64_t)(~key) << 32 | (of_key ? x & ((1u << of_index) - 1u) : x);
+      });
+    } else {
+      sort_items<uint64_t>(n, [](uint64_t item) { return item; }, [](uint64_t x) { return x; });
     }
-    int size = 32;
-    while (size < n) size <<= 1;
-    for (int i = n + threadIdx.x; i < size; i += kThreads) sh()->sorted[i] = ~0ull;
-    __syncthreads();
-#pragma unroll 1
-    for (int k = 2; k <= size; k <<= 1)
-#pragma unroll 1
-      for (int j = k >> 1; j > 0; j >>= 1) {
-#pragma unroll 1
-        for (int t = threadIdx.x; t < size / 2; t += kThreads) {
-          const int a = (t & ~(j - 1)) * 2 + (t & (j - 1)), b = a + j;
-          const uint64_t x = sh()->sorted[a], y = sh()->sorted[b];
-          if ((x > y) == ((a & k) == 0)) {
-            sh()->sorted[a] = y;
-            sh()->sorted[b] = x;
-          }
-        }
-        __syncthreads();
-      }
   }
-  // The last of the sorted list before which less than the aim lies; returns whether that is so for every aim within `unsure`.
-  // `from_end`: the aim is against the list's sum.
+  // Four neighbouring items a thread, or one: partners lie in the same thread, the same warp or, farther away, in shared memory.
+  template <typename K, typename Pack, typename Unpack>
+  __device__ __forceinline__ void sort_items(int n, Pack pack, Unpack unpack) {
+    static_assert(kList <= 4 * kThreads, "items of a thread");
+    if (n <= kThreads)
+      sort_by<K, 1>(n, pack, unpack);
+    else
+      sort_by<K, 4>(n, pack, unpack);
+  }
+  template <typename K, int kOwn, typename Pack, typename Unpack>
+  __device__ __forceinline__ void sort_by(int n, Pack pack, Unpack unpack) {
+    K *const items = reinterpret_cast<K *>(sh()->sorted);
+    const int i0 = threadIdx.x * kOwn;
+    K x[kOwn];
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) x[q] = i0 + q < n ? pack(sh()->sorted[i0 + q]) : ~(K)0;
+    int size = 32 * kOwn;
+    while (size < n) size <<= 1;
+    const bool in = (i0 & ~(32 * kOwn - 1)) < size;
+    const auto swap = [](K &a, K &b, bool rising) {
+      const K least = a < b ? a : b, most = a < b ? b : a;
+      a = rising ? least : most, b = rising ? most : least;
+    };
+#pragma unroll 1
+    for (int k = 2; k <= size; k <<= 1) {
+#pragma unroll 1
+      for (int j = k >> 1; j >= kOwn; j >>= 1) {
+        const bool small = ((i0 & j) == 0) == ((i0 & k) == 0);  // the thread's items take the smaller of the two
+        K y[kOwn];
+        if (j >= 32 * kOwn) {
+          __syncthreads();
+#pragma unroll
+          for (int q = 0; q < kOwn; ++q)
+            if (in) items[i0 + q] = x[q];
+          __syncthreads();
+#pragma unroll
+          for (int q = 0; q < kOwn; ++q) y[q] = in ? items[(i0 ^ j) + q] : x[q];
+        } else {
+#pragma unroll
+          for (int q = 0; q < kOwn; ++q) y[q] = __shfl_xor_sync(0xffffffffu, x[q], j / kOwn);
+        }
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) x[q] = small ? (x[q] < y[q] ? x[q] : y[q]) : (x[q] < y[q] ? y[q] : x[q]);
+      }
+      if constexpr (kOwn == 4) {
+        if (k >= 4) {
+          swap(x[0], x[2], (i0 & k) == 0);
+          swap(x[1], x[3], (i0 & k) == 0);
+        }
+        swap(x[0], x[1], (i0 & k) == 0);
+        swap(x[2], x[3], ((i0 + 2) & k) == 0);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q)
+      if (i0 + q < n) sh()->sorted[i0 + q] = unpack(x[q]);
+    __syncthreads();
+  }
+  // The last of the sorted list before which less than the aim lies, and whether that is so for every aim within `unsure`: kClear;
+  // kNear, not; kOutside, the cut need not be in the list at all.  `from_end`: the aim is against the list's sum.
   enum Border { kClear, kNear, kOutside };
   __device__ Border cut_from_list(bool weights, int n, double aim, bool from_end, double unsure, int &last) {
     constexpr int kOwn = kList / kThreads;
@@ -1395,7 +1520,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
     } else {
       bool whole = row.cut_v == kLowest;  // nothing is cut: the sums of the first sweep are those of what is kept
       typename Row<T>::Sums have = Row<T>::kStale;
-      double kept_unsure = 0.0;
 #pragma unroll 1
       for (int step = 0; step < 2; ++step) {  // top_k, then top_p
         const bool weights = step == 1;
@@ -1406,7 +1530,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
           share = top_p;
           all = rest + 1.0;
           if (whole)
-            unsure = row.eps(all) * all;
+            unsure = row.error(all);
           else
             all = row.sum(row.of_kept(kLowest)).all;
           // logits whose weight is under a V-th of 0.03 (1 - top_p) of the whole hold less than that much together
@@ -1416,33 +1540,40 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
         } else {
           floor = row.floor_of(top_k);
         }
-        have = row.select(weights, share, all, unsure, floor, below, kept_unsure, count);
+        have = row.select(weights, share, all, unsure, floor, below, count);
         whole = false;
       }
-      // by the warps' float32 sums where nothing is cut, unless the border is too near for them
+      // by float32's sums of the first sweep, of what is kept or of all where nothing is cut, unless the border is too near for them
+      const bool was_whole = whole;
+      if (whole) {
+        have = Row<T>::kTail;
+        count = (int)p.V - masked;
+      }
       double all;
       id = kNoIndex;
-      const bool was_whole = whole;
 #pragma unroll 1
       while (id == kNoIndex) {
-        double unsure = 0.0;
-        if (whole || have != Row<T>::kStale) {
+        double unsure = 0.0, behind = 0.0;
+        if (have != Row<T>::kStale) {
           all = row.sum_of_chunks();
-          unsure = have == Row<T>::kExact ? 0.0 : 2.0 * (whole ? row.eps(all) * all : kept_unsure);
-          if (whole) count = (int)p.V - masked;
           // a logarithm near zero wants all of its sum's digits
-          if (have == Row<T>::kTail && !(all > 1.5)) {
+          if (have == Row<T>::kTail && !was_whole && !(all > 1.5)) {
             have = Row<T>::kStale;
             continue;
+          }
+          if (have == Row<T>::kTail) {
+            // Of a sum P in front of the token and S behind it, u (P + S) is off by as much of P's error as P itself but for 1 - u of
+            // it, and by u of S's.  What is below float32's range is in the last term
+            behind = was_whole ? 0.0 : fmax(0.0, rest + 1.0 - all);
+            unsure = (1.0 - u) * row.error(u * all + behind) + u * row.error((1.0 - u) * all + behind) + row.error(behind) + 1e-12 * all;
           }
         } else {
           const typename Row<T>::Sum r = row.sum(row.of_kept(kLowest));
           all = r.all;
           count = r.n;
         }
-        id = row.found(row.of_kept(kLowest), (double)u * all, unsure, false, whole ? 1 : have == Row<T>::kTail ? 2 : 0);
+        id = row.found(row.of_kept(kLowest), (double)u * all, unsure, false, have, behind);
         if (id == kNoIndex) have = Row<T>::kStale;
-        whole = false;
       }
       kept_rest = was_whole ? rest : all - 1.0;
     }
@@ -1467,11 +1598,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
 
 // ---- host --------------------------------------------------------------------------------------------------------------
 
-// Blocks that share a row: as many as the chip has room for beside the other rows, while each has work.
+// Blocks that share a row.  More of them shorten the sweeps and lengthen what they do together, and clusters of eight find room
+// for fewer of them at a time.  1 / 2 / 4 / 8 blocks a row, us a call, of bfloat16:
+//   4 x 151,936, top_p 0.95    110 / 78 / 55 / 51       74 x 151,936, top_p 0.95   226 / 142 / 127 / 185
+//   64 x 151,936, nothing cut   71 / 52 / 36 / 42       148 x 151,936, top_k 50     65 / 76 / 171 / 287
+//   16 x 32,768, top_p 0.95     55 / 53 / 48 / 51       16 x 8,192, top_k 50        34 / 41 / 41 / 52
+// so two where the chip holds them all, four and eight where that leaves room, and as long as each has 16 KB.
 inline int choose_blocks(long long T, long long row_bytes) {
-  int log_blocks = 0;
-  while (log_blocks < 3 && (T << (log_blocks + 1)) <= 296 && (row_bytes >> (log_blocks + 1)) >= 16 * 1024) ++log_blocks;
-  return log_blocks;
+  const auto room = [&](int blocks, long long most) { return T * blocks <= most && row_bytes >= blocks * 16LL * 1024; };
+  return room(8, 128) ? 3 : room(4, 256) ? 2 : room(2, 296) ? 1 : 0;
 }
 
 template <typename T>
