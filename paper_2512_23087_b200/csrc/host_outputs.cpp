@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/DynamicTypes.h>
@@ -427,6 +428,11 @@ PyObject *rms_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args
     workspace = make(h, {static_cast<int64_t>(std::max<size_t>(bytes(DVP_ENTRY_RMS_NORM_BACKWARD, &a), 256))}, at::kByte);
   }
   a.workspace = workspace.data_ptr();
+  // its memory stays put until the stream is through with it, though nobody holds the tensor
+  if (!given(args[9]) && given(args[10]))
+    c10::cuda::CUDACachingAllocator::recordStream(
+        workspace.storage().data_ptr(),
+        c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(PyLong_AsVoidPtr(args[10])), static_cast<c10::DeviceIndex>(h.get_device())));
   a.workspace_bytes = static_cast<size_t>(workspace.numel() * workspace.element_size());
   a.stream = stream_of(args[10], h.get_device());
   THPObjectPtr d(PyDict_New());

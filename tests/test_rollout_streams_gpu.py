@@ -1,0 +1,54 @@
+"""Calls on a stream of the caller's own: what a call allocates for itself must not be handed out again while that stream works."""
+import pytest
+import torch
+
+from paper_2512_23087_b200 import binding as b
+
+pytestmark = pytest.mark.gpu
+
+
+def _held():
+    """Bytes that nobody holds any more and that the allocator keeps back for a stream."""
+    s = torch.cuda.memory_stats()
+    return s["active_bytes.all.current"] - s["allocated_bytes.all.current"]
+
+
+def test_backward_workspace_outlives_the_call():
+    T, H = 2048, 1024  # large enough for storages of their own
+    h = torch.randn(T, H, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    w = torch.ones(H, device="cuda")
+    rstd = h.square().mean(1).rsqrt()
+    want = b.dvp_rms_norm_backward(h, h, w, rstd)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    before = _held()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    got = b.dvp_rms_norm_backward(h, h, w, rstd, stream=side)
+    held = _held() - before
+    torch.cuda.synchronize()
+    assert held >= 592 * H * 4
+    assert torch.equal(got.d_x, want.d_x) and torch.equal(got.d_weight, want.d_weight)
+
+
+@pytest.mark.parametrize("T", [2, 600])
+def test_rollout_head_keeps_its_hidden_states(T):
+    H, V = 2048, 1000
+    g = torch.Generator("cuda").manual_seed(2)
+    x = torch.randn(T, H, device="cuda", generator=g).bfloat16()
+    w = torch.randn(V, H, device="cuda", generator=g).bfloat16()
+    u, gamma = torch.rand(T, device="cuda", generator=g), torch.ones(H, device="cuda")
+    q = b.dvp_quantize_fp8(w)
+    want = b.dvp_rollout_head(x, gamma, q.q, q.scale, u)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    before = _held()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    got = b.dvp_rollout_head(x, gamma, q.q, q.scale, u, stream=side)
+    # a small call's rstd lies in the same storage as the hidden states and holds it
+    got.rstd = None
+    held = _held() - before
+    torch.cuda.synchronize()
+    assert held >= T * H
+    assert torch.equal(got.ids, want.ids) and torch.equal(got.logits, want.logits)
