@@ -581,17 +581,7 @@ struct Row {
       const int own = __popc(mask), up_to = warp_scan(own), all = __shfl_sync(0xffffffffu, up_to, 31);
       double of_piece = 0.0;
       int at = up_to - own;
-      if (a.rest == kNone && a.weights && all >= 16 * kPer) {
-        // most of them: as they lie
-#pragma unroll
-        for (int j = 0; j < kPer / 2; ++j) {
-          float lo, hi;
-          two_of<T>(w, j, lo, hi);
-          const double one = row.weight(lo), two = row.weight(hi);
-          of_piece += (mask >> (2 * j) & 1 ? one : 0.0) + (mask >> (2 * j + 1) & 1 ? two : 0.0);
-        }
-        n += own;
-      } else if (a.rest == kNone) {
+      if (a.rest == kNone) {
         // sums alone: two side by side, as one exponential is a long chain
 #pragma unroll
         for (int j = 0; j < kPer / 2; ++j) {
@@ -653,26 +643,29 @@ struct Row {
         acc += warp_sum(of_piece);
       }
     });
-    const bool first = a.rest == kFirst;
-    n = first ? __reduce_min_sync(0xffffffffu, best) : __reduce_add_sync(0xffffffffu, n);
+    return row.joined(acc, a.rest == kFirst ? best : n, a.rest == kFirst);
+  }
+  // The warps' sums to `chunk`, the blocks' to each other; `first`: the least of their n, else the sum.
+  __device__ __forceinline__ Sum joined(double acc, int n, bool first) {
+    n = first ? __reduce_min_sync(0xffffffffu, n) : __reduce_add_sync(0xffffffffu, n);
     __syncthreads();  // chunk and warp_n have been read
-    if (row.lane == 0) {
-      sh()->chunk[row.warp] = acc;
-      sh()->warp_n[row.warp] = (uint32_t)n;
+    if (lane == 0) {
+      sh()->chunk[warp] = acc;
+      sh()->warp_n[warp] = (uint32_t)n;
     }
     __syncthreads();
-    const int ns = (int)sh()->warp_n[row.lane & (kWarps - 1)];
-    n = first ? __reduce_min_sync(0xffffffffu, ns) : __reduce_add_sync(0xffffffffu, row.lane < kWarps ? ns : 0);
+    const int ns = (int)sh()->warp_n[lane & (kWarps - 1)];
+    n = first ? __reduce_min_sync(0xffffffffu, ns) : __reduce_add_sync(0xffffffffu, lane < kWarps ? ns : 0);
     Sum r;
-    r.all = warp_sum(row.lane < kWarps ? sh()->chunk[row.lane & (kWarps - 1)] : 0.0);
+    r.all = warp_sum(lane < kWarps ? sh()->chunk[lane & (kWarps - 1)] : 0.0);
     r.n = n;
-    if (row.blocks > 1) {
-      row.turn ^= 1;
-      if (threadIdx.x == 0) sh()->slot[row.turn] = Slot{r.all, 0.f, n};
-      row.meet();
-      const Slot o = row.told(row.lane & (row.blocks - 1));
-      r.all = warp_sum(row.lane < row.blocks ? o.a : 0.0);
-      r.n = first ? __reduce_min_sync(0xffffffffu, o.i) : __reduce_add_sync(0xffffffffu, row.lane < row.blocks ? o.i : 0);
+    if (blocks > 1) {
+      turn ^= 1;
+      if (threadIdx.x == 0) sh()->slot[turn] = Slot{r.all, 0.f, n};
+      meet();
+      const Slot o = told(lane & (blocks - 1));
+      r.all = warp_sum(lane < blocks ? o.a : 0.0);
+      r.n = first ? __reduce_min_sync(0xffffffffu, o.i) : __reduce_add_sync(0xffffffffu, lane < blocks ? o.i : 0);
     }
     return r;
   }
@@ -706,8 +699,35 @@ struct Row {
     }
     return v;
   }
-  // The whole row's, in double.
-  __device__ __forceinline__ double whole() { return sum(Pass{kLowest, kNoIndex, -kNegInf, kNegInf, true, kNone, 0, 0}).all; }
+  // The whole row's, in double, with nothing to leave out: a logit of -inf has no weight by itself.  Many exponentials side by side, since
+  // one is a long chain (151,936 logits by one block of an SM: 46 us, as a pass 80).
+  __device__ __noinline__ static Sum sweep_whole(Row row) {
+    double *parts = sh()->part[row.warp];
+    for (int q = row.lane; q < kParts; q += 32) parts[q] = 0.0;
+    __syncwarp();
+    double acc = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < row.mine; ++i) {
+      uint32_t w[8];
+      row.load(row.first + i, w);
+      double of_piece = 0.0;
+#pragma unroll
+      for (int j = 0; j < kPer / 2; ++j) {
+        float lo, hi;
+        two_of<T>(w, j, lo, hi);
+        of_piece += row.weight(lo) + row.weight(hi);
+      }
+      of_piece = warp_sum(of_piece);
+      if (row.lane == 0) parts[i >> row.log_q] += of_piece;
+      acc += of_piece;
+    }
+    return row.joined(acc, 0, false);
+  }
+  __device__ __forceinline__ double whole() {
+    const double all = sweep_whole(*this).all;
+    if (blocks > 1) turn ^= 1;  // as the sweep has told the blocks
+    return all;
+  }
 
   // The index at which the running sum of a pass `a` over the row passes `aim`, where the warps' parts lie in `chunk` and the blocks'
   // have been told: the first that it looks for where it does, or the last of those with something where rounding leaves none.
@@ -1567,6 +1587,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
             behind = was_whole ? 0.0 : fmax(0.0, rest + 1.0 - all);
             unsure = (1.0 - u) * row.error(u * all + behind) + u * row.error((1.0 - u) * all + behind) + row.error(behind) + 1e-12 * all;
           }
+        } else if (was_whole) {
+          all = row.whole();
         } else {
           const typename Row<T>::Sum r = row.sum(row.of_kept(kLowest));
           all = r.all;
