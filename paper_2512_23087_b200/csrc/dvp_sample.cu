@@ -19,7 +19,7 @@
 // is tried first: it is good to error(), and mostly nothing lies so near the border that this matters.  With few rows the blocks
 // of a cluster share a row and exchange sums through shared memory.
 //
-// Bound by instruction issue and by the chain of a row's phases, not by HBM: 1,024 rows of 151,936 bfloat16 (311 MB, 47 us at 6.6 TB/s)
+// Bound by instruction issue (three cycles of five) and by the waits of a row's phases, not by HBM: 1,024 rows of 151,936 bfloat16 (311 MB, 47 us at 6.6 TB/s)
 // take 123 us for the largest logit, 177 with nothing cut, 335 with a min-p set of 80 % of the row, 317 with top_k 50 and 533 with
 // top_p 0.95, whose rows are read four times, once only a quarter of them.  Of a top_p row's some 200 thousand cycles, two
 // rows an SM, the first sweep has 50, the quarter's histogram and its window 33, the sum behind the window with its list 80, the sort
