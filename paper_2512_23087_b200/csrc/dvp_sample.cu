@@ -20,7 +20,7 @@
 // of a cluster share a row and exchange sums through shared memory.
 //
 // Bound by instruction issue (three cycles of five) and by the waits of a row's phases, not by HBM: 1,024 rows of 151,936 bfloat16 (311 MB, 47 us at 6.6 TB/s)
-// take 123 us for the largest logit, 177 with nothing cut, 335 with a min-p set of 80 % of the row, 317 with top_k 50 and 533 with
+// take 122 us for the largest logit, 173 with nothing cut, 334 with a min-p set of 80 % of the row, 307 with top_k 50 and 529 with
 // top_p 0.95, whose rows are read four times, once only a quarter of them.  Of a top_p row's some 200 thousand cycles, two
 // rows an SM, the first sweep has 50, the quarter's histogram and its window 33, the sum behind the window with its list 80, the sort
 // 20.  One row of that length takes 19 to 50 us by eight blocks.
@@ -1203,16 +1203,15 @@ struct Row {
       __syncwarp();
       waiting = 0;
     };
-    uint32_t next[2][8];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      if (u < mine) load(first + u, next[u]);
+    // one piece on its way (1,024 rows, top_p 0.95: 529 us; two 533, three 607, for want of registers)
+    uint32_t next[8];
+    if (mine > 0) load(first, next);
 #pragma unroll 1
     for (int i = 0; i < mine; ++i) {
       uint32_t w[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = next[0][j], next[0][j] = next[1][j];
-      if (i + 2 < mine) load(first + i + 2, next[1]);
+      for (int j = 0; j < 8; ++j) w[j] = next[j];
+      if (i + 1 < mine) load(first + i + 1, next);
       const unsigned from_low = from(w, low), in = from_low & ~over(w, high);
       n_not += __popc(from_low);
       float g;
