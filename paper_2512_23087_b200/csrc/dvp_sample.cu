@@ -313,6 +313,8 @@ struct Row {
             const double f = power(((double)tm - (double)top) * inv_t);
             s = (s + (double)n) * f;
             of_part *= (float)f;
+          } else {
+            of_part = 0.f;  // as n, it has counted what is -inf so far as the largest
           }
           n = 0.f;
           tm = top;
