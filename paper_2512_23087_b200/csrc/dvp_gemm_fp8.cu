@@ -12,9 +12,8 @@
 #include <cmath>
 
 #include "dvp_common.cuh"
+#include "dvp_fp8.cuh"
 #include "dvp_tensor.cuh"
-
-#include <cuda_fp8.h>
 
 namespace dvp {
 namespace fp8 {
@@ -501,7 +500,7 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T *x, long long ld_
   const long long rb = blockIdx.x % row_blocks, cb = blockIdx.x / row_blocks;
   const long long c = cb * kBlock + lane * 4, r0 = rb * 128 + warp * 16;
   const bool whole = vec && c + 4 <= cols;
-  float v[16][4], least = 1.262177448e-29f /* 2^-96 */, amax = least;
+  float v[16][4], amax = kLeastAmax;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
 #pragma unroll
@@ -540,26 +539,25 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T *x, long long ld_
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) amax = fmaxf(amax, part[i]);
-    if (threadIdx.x == 0) scale[rb * ld_scale + cb] = amax / 448.f;
+    if (threadIdx.x == 0) scale[rb * ld_scale + cb] = scale_of(amax);
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const long long r = r0 + i;
     if (r >= rows) break;
     if constexpr (kRowScale) {
-      amax = warp_max(fmaxf(fmaxf(fmaxf(fabsf(v[i][0]), fabsf(v[i][1])), fmaxf(fabsf(v[i][2]), fabsf(v[i][3]))), least));
-      if (lane == 0) scale[r * ld_scale + cb] = amax / 448.f;
+      amax = warp_max(fmaxf(fmaxf(fmaxf(fabsf(v[i][0]), fabsf(v[i][1])), fmaxf(fabsf(v[i][2]), fabsf(v[i][3]))), kLeastAmax));
+      if (lane == 0) scale[r * ld_scale + cb] = scale_of(amax);
     }
-    const float inv = 1.f / (amax / 448.f);
-    uint32_t q = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[i][0] * inv, v[i][1] * inv), __NV_SATFINITE, __NV_E4M3);
-    q |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[i][2] * inv, v[i][3] * inv), __NV_SATFINITE, __NV_E4M3) << 16;
+    uint32_t q[1];
+    quotients<4>(v[i], scale_of(amax), q);
     uint8_t *o = out + r * ld_out + c;
     if (whole) {
-      *reinterpret_cast<uint32_t *>(o) = q;
+      *reinterpret_cast<uint32_t *>(o) = q[0];
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (c + j < cols) o[j] = (uint8_t)(q >> (8 * j));
+        if (c + j < cols) o[j] = (uint8_t)(q[0] >> (8 * j));
     }
   }
 }

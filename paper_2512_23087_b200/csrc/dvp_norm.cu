@@ -11,16 +11,13 @@
 #include <cmath>
 
 #include "dvp_common.cuh"
-
-#include <cuda_fp8.h>
+#include "dvp_fp8.cuh"
 
 namespace dvp {
 namespace norm {
 
 constexpr int kBlockCols = 128;  // columns that share a scale
 constexpr int kVec = 8;          // elements of a vector: 16 bytes of a 16-bit type, 32 of float32, 8 of e4m3
-constexpr float kFp8Max = 448.f;
-constexpr float kLeastAmax = 1.262177448e-29f;  // 2^-96: a block of zeros has a scale that can be divided by
 constexpr int kMaxPartials = 592;               // rows of partial sums of dw: four blocks an SM
 
 struct Params {
@@ -89,10 +86,6 @@ __device__ __forceinline__ float load_weight(const void *w, int w_f32, long long
   return sizeof(T) == 4 || w_f32 ? __ldg(static_cast<const float *>(w) + c) : Storage<T>::widen(__ldg(static_cast<const T *>(w) + c));
 }
 
-__device__ __forceinline__ uint32_t fp8_pair(float lo, float hi) {
-  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
-}
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -122,17 +115,10 @@ __device__ __forceinline__ float row_sum(float v, int tpr, float *part) {
   return s;
 }
 
-// Reciprocals and roots as the special-function unit gives them, to 2^-22.
-__device__ __forceinline__ float approx_rcp(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
 // ---- rows in vectors ---------------------------------------------------------------------------------------------------
 
 // A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: the next is on its way while one is summed up and stored, so that loads
-// never pause (16,384 x 4,096 bfloat16 to 8 bits: 103 us, with one row a block and nothing on its way 139).
+// never pause (16,384 x 4,096 bfloat16 to 8 bits, quotients aside: 103 us, with one row a block and nothing on its way 139).
 template <typename T, typename TOut, int kPer>
 __global__ void __launch_bounds__(kPer == 4 ? 512 : 256, kPer == 1 ? 4 : kPer == 2 ? 3 : 1) rms_norm_kernel(const Params p, const int tpr) {
   __shared__ __align__(16) float part[2][32];
@@ -206,18 +192,17 @@ __global__ void __launch_bounds__(kPer == 4 ? 512 : 256, kPer == 1 ? 4 : kPer ==
       for (int j = 0; j < kVec; ++j) y[j] = h[i][j] * s * w[j];
       if constexpr (sizeof(TOut) == 1) {
         // sixteen neighbouring lanes hold a block of 128 columns
-        float a = kLeastAmax;
+        float a = fp8::kLeastAmax;
 #pragma unroll
         for (int j = 0; j < kVec; ++j) a = fmaxf(a, fabsf(y[j]));
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        const float scale = a * (1.f / kFp8Max), inv = approx_rcp(scale);
+        const float scale = fp8::scale_of(a);
         if (here) {
           if ((threadIdx.x & 15) == 0) p.scale[t * p.ld_scale + column(i) / kBlockCols] = scale;
-          uint2 q;
-          q.x = fp8_pair(y[0] * inv, y[1] * inv) | fp8_pair(y[2] * inv, y[3] * inv) << 16;
-          q.y = fp8_pair(y[4] * inv, y[5] * inv) | fp8_pair(y[6] * inv, y[7] * inv) << 16;
-          st_stream8(y_at + i * across, q);
+          uint32_t q[2];
+          fp8::quotients<kVec>(y, scale, q);
+          st_stream8(y_at + i * across, make_uint2(q[0], q[1]));
         }
       } else if (here) {
         store8(y_at + i * across, y);
@@ -268,7 +253,7 @@ __global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params 
     const float s = rsqrtf(fmaf(block_sum(sum, part), p.inv_h, p.eps));
     if (threadIdx.x == 0 && p.rstd) p.rstd[t] = s;
     for (long long b = warp; b < blocks; b += kWarps) {
-      float h[4], y[4], a = kLeastAmax;
+      float h[4], y[4], a = fp8::kLeastAmax;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const long long c = column(b, j);
@@ -276,12 +261,12 @@ __global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params 
         y[j] = c < p.H ? h[j] * s * load_weight<T>(p.w, p.w_f32, c) : 0.f;
         a = fmaxf(a, fabsf(y[j]));
       }
-      float inv = 1.f;
+      uint32_t q[1] = {0};
       if constexpr (sizeof(TOut) == 1) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        const float scale = a * (1.f / kFp8Max);
-        inv = approx_rcp(scale);
+        const float scale = fp8::scale_of(a);
+        fp8::quotients<4>(y, scale, q);
         if (lane == 0) p.scale[t * p.ld_scale + b] = scale;
       }
 #pragma unroll
@@ -290,7 +275,7 @@ __global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params 
         if (c >= p.H) continue;
         if (p.r_out) static_cast<T *>(p.r_out)[t * p.ld_r_out + c] = Storage<T>::narrow(h[j]);
         if constexpr (sizeof(TOut) == 1)
-          static_cast<uint8_t *>(p.out)[t * p.ld_out + c] = (uint8_t)__nv_cvt_float_to_fp8(y[j] * inv, __NV_SATFINITE, __NV_E4M3);
+          static_cast<uint8_t *>(p.out)[t * p.ld_out + c] = (uint8_t)(q[0] >> (8 * j));
         else
           static_cast<TOut *>(p.out)[t * p.ld_out + c] = Storage<TOut>::narrow(y[j]);
       }
@@ -453,7 +438,7 @@ inline bool weight_vectors(const void *w) { return (uintptr_t)w % 16 == 0; }
 struct Shape {
   int per, tpr, rpb;  // vectors a thread, threads a row, rows a block
 };
-// Forward, one vector a thread up to 256 threads a row, then two (16,384 x 4,096 to 8 bits: 103 us, one vector and 512 threads
+// Forward, one vector a thread up to 256 threads a row, then two (16,384 x 4,096 to 8 bits, quotients aside: 103 us, one vector and 512 threads
 // 114), then four; backward, whose threads hold a row of dw too, 512.  per = 0: too long for the registers, or no vector at all.
 inline Shape shape_of(long long H, bool backward) {
   const long long nv = H / kVec;
