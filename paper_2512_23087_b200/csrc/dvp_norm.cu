@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kPer == 4 ? 512 : 256, kPer == 1 ? 4 : kPer ==
 #pragma unroll
       for (int i = 0; i < kPer; ++i) x[a][i] = x[a + 1][i], r[a][i] = r[a + 1][i];
     if (first + kAhead * step < p.T) fetch(x[kAhead - 1], r[kAhead - 1], t + kAhead * step < p.T);
-    const float s = rsqrtf(fmaf(row_sum(sum, tpr, part[turn]), p.inv_h, p.eps));  // two sets: see the backward kernel
+    const float s = 1.f / sqrtf(fmaf(row_sum(sum, tpr, part[turn]), p.inv_h, p.eps));  // two sets: see the backward kernel
     if (live && lane_of_row == 0 && p.rstd) p.rstd[t] = s;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params 
         const float v = c < p.H ? entry(c) : 0.f;
         sum = fmaf(v, v, sum);
       }
-    const float s = rsqrtf(fmaf(block_sum(sum, part), p.inv_h, p.eps));
+    const float s = 1.f / sqrtf(fmaf(block_sum(sum, part), p.inv_h, p.eps));
     if (threadIdx.x == 0 && p.rstd) p.rstd[t] = s;
     for (long long b = warp; b < blocks; b += kWarps) {
       float h[4], y[4], a = fp8::kLeastAmax;
