@@ -507,7 +507,8 @@ int dvp_row_wait_status(uint32_t *status_out);
  * --debug-bounds gives libdvp_b200_bounds.so).  In that build an index out of range
  * is never used: the access is skipped and a code is OR-ed into a per-device word
  * (1 granule-bound table, 2 hot list, 4 granule index, 8 global offset, 16 candidate
- * ring, 32 candidate list, 64 resident slot).  This call waits for all work on the
+ * ring, 32 candidate list, 64 resident slot; 128: dvp_sample took sums that were no
+ * longer those that it looked for).  This call waits for all work on the
  * current device, copies the word to *status_out (a host pointer) and clears it; 0
  * means that no check has failed since the last call.  The ordinary build has no
  * checks and returns DVP_ERR_UNSUPPORTED.  The paper has no counterpart: it stands

@@ -38,7 +38,8 @@ enum : unsigned {
   DVP_OOB_GLOBAL = 8,   // global element offset outside the row
   DVP_OOB_RING = 16,    // candidate ring slot
   DVP_OOB_LIST = 32,    // candidate list entry
-  DVP_OOB_SLOT = 64     // resident-row slot or its bytes
+  DVP_OOB_SLOT = 64,    // resident-row slot or its bytes
+  DVP_STALE_SUMS = 128  // a draw by sums that another pass has replaced
 };
 #ifdef DVP_DEBUG_BOUNDS
 struct BoundsCtx {

@@ -54,6 +54,7 @@ struct Params {
   long long T, V, ld;
   int id_is_i32, log_blocks;
   int bounds;  // granules of a block's part whose maxima are held, 0: too many
+  unsigned int *bounds_status;  // the bounds-checking build's status word; unused otherwise
 };
 
 // What a block tells the others of its row.
@@ -199,6 +200,14 @@ struct Row {
   // what is kept so far
   float cut_v;
   int cut_i;
+#ifdef DVP_DEBUG_BOUNDS
+  bool replaced = false;  // the first sweep's sums: a pass has put its own in their place
+#endif
+  __device__ __forceinline__ void replace() {
+#ifdef DVP_DEBUG_BOUNDS
+    replaced = true;
+#endif
+  }
 
   // The block's shared memory, by its own name wherever it is used: through a pointer that is handed on, every access would be one of
   // the general kind.
@@ -680,6 +689,7 @@ struct Row {
   __device__ __forceinline__ Sum sum(const Pass &a) {
     const Sum r = pass(*this, a);
     if (blocks > 1) turn ^= 1;  // as the pass has told the blocks
+    replace();
     return r;
   }
   // The histogram of the distances of what is kept, none below `low`: most of a row's logits, one by one.
@@ -734,6 +744,7 @@ struct Row {
   __device__ __forceinline__ double whole() {
     const double all = sweep_whole(*this).all;
     if (blocks > 1) turn ^= 1;  // as the sweep has told the blocks
+    replace();
     return all;
   }
 
@@ -844,6 +855,9 @@ struct Row {
   }
   // find(), and whether it failed, known to all blocks; `everywhere`: the index too.
   __device__ __forceinline__ int found(const Pass &a, double aim, double unsure, bool everywhere, Sums have, double behind) {
+#ifdef DVP_DEBUG_BOUNDS
+    bounds_ok(have == kTail && replaced ? 1 : 0, 1, DVP_STALE_SUMS);
+#endif
     int at = find(*this, a, aim, unsure, have, behind);
     if ((everywhere || unsure > 0.0) && blocks > 1) {
       tell(0.0, 0.f, at);
@@ -902,7 +916,8 @@ struct Row {
   // Moves the cut to the last logit, in falling order, before which less than share * all lies; weights: sums of weights, else
   // of ones.  Logits below `floor` are known to lie behind it.  `all`: the amount in the whole row, good to `unsure`, of which at
   // most `below` lies below `floor`.  Returns what `chunk` and the parts have then, with `n_kept` the number that is kept: kTail, the
-  // first sweep's parts and `tail` of them what is not kept; kExact, sums of what is kept in double; kStale.
+  // first sweep's parts and `tail` of them what is not kept; kExact, sums of what is kept in double; kStale, neither, and `n_kept` is
+  // left to whoever forms them.
   __device__ Sums select(bool weights, double share, double all, double unsure, float floor, double below, int &n_kept) {
     double aim = share * all;
     const float span = floor > 0.5f * kLowest ? m - floor : (float)(40.0 / inv_t);
@@ -914,6 +929,7 @@ struct Row {
     // of them guesses where the cut is, and what is found there shows whether it was right (1,024 rows, top_p 0.95: from all pieces
     // 891 us, an eighth of them 847, whose windows are wider, a quarter 709).
     bool guess = unsure > 0.0 && all_segs >= 16 * kWarps * blocks;
+    bool replaced = false;  // the first sweep's sums: a pass has put its own in their place
     if (guess) {
       for (int i = threadIdx.x; i < kBins; i += kThreads) sh()->hist[i] = 0;
       __syncthreads();
@@ -961,6 +977,7 @@ struct Row {
         tail = b.sum, n_not = b.n_not;
       } else {
         sums = sum(a);
+        replaced = true;
         above = weights ? sums.all : (double)sums.n;
       }
       if (ties) {
@@ -1013,7 +1030,7 @@ struct Row {
             level = -1;
             continue;
           }
-          have = kTail;
+          have = replaced ? kStale : kTail;  // what lies behind says what is kept of the first sweep's sums, and only of them
           if (at != kClear) {
             for (int i = threadIdx.x; i < n; i += kThreads) sh()->list[i] = sh()->sorted[i];  // passes take their place
             __syncthreads();
@@ -1031,7 +1048,7 @@ struct Row {
           cut_from_list(weights, n, aim - above, false, 0.0, last);
         }
         set_cut(last);
-        {
+        if (have != kStale) {
           // The list's logits: those behind the cut go to the tail, or the kept ones to the exact sums, of the warp that has their
           // pieces and of their part.
           // Whole numbers of 2^-52 of the largest are added, in any order.
@@ -1491,6 +1508,7 @@ struct Row {
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
+  DVP_BOUNDS_BEGIN(p.bounds_status);
   Row<T> row;
   row.bounded = p.bounds != 0;
   row.warp = threadIdx.x >> 5;
@@ -1689,7 +1707,7 @@ extern "C" int dvp_sample(const dvp_sample_args *a) {
   if (a->T == 0) return DVP_OK;
   if (!a->logits || !a->uniform || !a->ids) return DVP_ERR_INVALID_ARG;
   Params p{a->logits, a->uniform, a->temperature_rows, a->top_p_rows, a->rho_rows, a->top_k_rows, a->temperature, a->top_p, a->rho,
-           a->top_k, a->ids, a->logp, a->logp_mp, a->count, a->T, a->V, a->ld, a->id_dtype == DVP_ID_I32, 0, 0};
+           a->top_k, a->ids, a->logp, a->logp_mp, a->count, a->T, a->V, a->ld, a->id_dtype == DVP_ID_I32, 0, 0, dvp::bounds_status_word()};
   const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
   const cudaError_t e = a->logits_dtype == DVP_F32    ? launch<float>(a, p, stream)
                         : a->logits_dtype == DVP_BF16 ? launch<__nv_bfloat16>(a, p, stream)
