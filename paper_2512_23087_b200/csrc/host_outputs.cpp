@@ -266,6 +266,13 @@ bool given(PyObject *o) { return o != Py_None; }
 void *stream_of(PyObject *o, int device) {
   return given(o) ? PyLong_AsVoidPtr(o) : static_cast<void *>(c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream());
 }
+// What the call makes for itself stays put until the stream that the caller has named is through with it, whoever lets go of it before.
+void keep_for(const at::Tensor &t, PyObject *stream) {
+  if (given(stream) && t.numel() > 0)
+    c10::cuda::CUDACachingAllocator::recordStream(
+        t.storage().data_ptr(), c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(PyLong_AsVoidPtr(stream)),
+                                                                 static_cast<c10::DeviceIndex>(t.get_device())));
+}
 void same_device(const at::Tensor &like, const at::Tensor &x, const char *name) {
   if (x.device() != like.device()) refuse(PyExc_ValueError, "%s must live on the device of the others", name);
 }
@@ -428,11 +435,7 @@ PyObject *rms_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args
     workspace = make(h, {static_cast<int64_t>(std::max<size_t>(bytes(DVP_ENTRY_RMS_NORM_BACKWARD, &a), 256))}, at::kByte);
   }
   a.workspace = workspace.data_ptr();
-  // its memory stays put until the stream is through with it, though nobody holds the tensor
-  if (!given(args[9]) && given(args[10]))
-    c10::cuda::CUDACachingAllocator::recordStream(
-        workspace.storage().data_ptr(),
-        c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(PyLong_AsVoidPtr(args[10])), static_cast<c10::DeviceIndex>(h.get_device())));
+  if (!given(args[9])) keep_for(workspace, args[10]);
   a.workspace_bytes = static_cast<size_t>(workspace.numel() * workspace.element_size());
   a.stream = stream_of(args[10], h.get_device());
   THPObjectPtr d(PyDict_New());
@@ -478,6 +481,7 @@ PyObject *gemm_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   const int32_t code = code_of(type, "out");
   if (!out.defined()) out = make(x, {M, N}, type);
   const at::Tensor status = M && N ? make(x, {1}, at::kInt) : at::zeros({1}, x.options().dtype(at::kInt).requires_grad(false));
+  keep_for(status, args[7]);  // callers let go of it at once
   dvp_gemm_fp8_args a = {};
   a.struct_size = sizeof(a);
   a.c_dtype = code;

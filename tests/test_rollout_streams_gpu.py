@@ -52,3 +52,29 @@ def test_rollout_head_keeps_its_hidden_states(T):
     torch.cuda.synchronize()
     assert held >= T * H
     assert torch.equal(got.ids, want.ids) and torch.equal(got.logits, want.logits)
+
+
+def _product(M=8, K=256, N=1000):
+    g = torch.Generator("cuda").manual_seed(4)
+    a, w = (b.dvp_quantize_fp8(torch.randn(r, K, device="cuda", generator=g), block_rows=n) for r, n in ((M, 1), (N, 128)))
+    return a.q, a.scale, w.q, w.scale
+
+
+@pytest.mark.parametrize("M", [8, 100])
+def test_product_status_is_nobody_elses_while_the_stream_works(M):
+    """The status word is let go of at once, and what takes its place on the current stream must stay as it is."""
+    args = _product(M)
+    want, _ = b.dvp_gemm_fp8(*args)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    before = _held()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    got, status = b.dvp_gemm_fp8(*args, stream=side)
+    del status
+    held = _held() - before
+    words = [torch.full((1,), 77, dtype=torch.int32, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    assert [int(v) for v in words] == [77] * 8
+    assert held > 0
+    assert torch.equal(got, want)
