@@ -480,8 +480,15 @@ PyObject *gemm_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   const at::ScalarType type = given(args[6]) ? out.scalar_type() : type_of(args[5]);
   const int32_t code = code_of(type, "out");
   if (!out.defined()) out = make(x, {M, N}, type);
-  const at::Tensor status = M && N ? make(x, {1}, at::kInt) : at::zeros({1}, x.options().dtype(at::kInt).requires_grad(false));
+  const at::Tensor status = make(x, {1}, at::kInt);
   keep_for(status, args[7]);  // callers let go of it at once
+  if (M == 0 || N == 0) {  // no kernel runs that would say that none has given up
+    c10::cuda::OptionalCUDAStreamGuard on;
+    if (given(args[7]))
+      on.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(PyLong_AsVoidPtr(args[7])),
+                                                       static_cast<c10::DeviceIndex>(x.get_device())));
+    status.zero_();
+  }
   dvp_gemm_fp8_args a = {};
   a.struct_size = sizeof(a);
   a.c_dtype = code;

@@ -78,3 +78,18 @@ def test_product_status_is_nobody_elses_while_the_stream_works(M):
     assert [int(v) for v in words] == [77] * 8
     assert held > 0
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("M,N", [(0, 1000), (8, 0)])
+def test_an_empty_product_says_so_on_the_named_stream(M, N):
+    a, sa, w, sw = _product()
+    side = torch.cuda.Stream()
+    old = torch.full((1,), 77, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    del old     # what the status word finds in its place
+    torch.cuda._sleep(50_000_000)
+    _, status = b.dvp_gemm_fp8(a[:M], sa[:M], w[:N], sw[:-(-N // 128)], stream=side)
+    with torch.cuda.stream(side):
+        said = status.to("cpu", non_blocking=False)
+    torch.cuda.synchronize()
+    assert int(said) == 0
