@@ -897,9 +897,6 @@ def dvp_rollout_head(x: torch.Tensor, norm_weight: torch.Tensor, w_vocab: torch.
     head), ``residual``, ``rstd`` and ``status`` beside it."""
     n = dvp_rms_norm(x, norm_weight, residual=residual, eps=eps, out_dtype=torch.float8_e4m3fn, stream=stream)
     logits, status = dvp_gemm_fp8(n.y, n.scale, w_vocab, w_scale, out_dtype=logits_dtype, stream=stream)
-    if stream is not None:  # nobody holds the 8-bit hidden states while the stream reads them
-        n.y.record_stream(stream)
-        n.scale.record_stream(stream)
     res = dvp_sample(logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, rho=rho, id_dtype=id_dtype, stream=stream)
     res.logits, res.residual, res.rstd, res.status = logits, n.residual, n.rstd, status
     return res

@@ -371,7 +371,10 @@ PyObject *rms_norm(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   const bool make_h = !h.defined() && given(args[3]);
   Outputs made(x, Outputs::room(T, ld, out) + Outputs::room(T, 1, at::kFloat) + (fp8 ? Outputs::room(T, blocks, at::kFloat) : 0) +
                       (make_h ? Outputs::room(T, H, x.scalar_type()) : 0));
-  if (make_h) h = made.take(T, H, H, x.scalar_type());
+  if (make_h) {
+    h = made.take(T, H, H, x.scalar_type());
+    keep_for(h, args[7]);
+  }
   if (h.defined()) a.residual_out = h.data_ptr(), a.ld_residual_out = h.stride(0);
   const at::Tensor y = made.take(T, H, ld, out), rstd = made.take(T, -1, 0, at::kFloat);
   a.out = y.data_ptr(), a.ld_out = ld;
@@ -379,10 +382,13 @@ PyObject *rms_norm(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   if (fp8) {
     const at::Tensor scale = made.take(T, blocks, blocks, at::kFloat);
     a.scale = static_cast<float *>(scale.data_ptr()), a.ld_scale = blocks;
+    keep_for(scale, args[7]);
     put(d.get(), g_more.scale, THPVariable_Wrap(scale));
   } else {
     put(d.get(), g_more.scale, none());
   }
+  keep_for(y, args[7]);
+  keep_for(rstd, args[7]);
   put(d.get(), g_more.y, THPVariable_Wrap(y));
   put(d.get(), g_more.rstd, THPVariable_Wrap(rstd));
   put(d.get(), g_more.residual, h.defined() ? THPVariable_Wrap(h) : none());

@@ -93,3 +93,44 @@ def test_an_empty_product_says_so_on_the_named_stream(M, N):
         said = status.to("cpu", non_blocking=False)
     torch.cuda.synchronize()
     assert int(said) == 0
+
+
+def _behind_a_busy_stream(call):
+    """Lets go of a call's results while its stream is held back, but for what `call` returns: the bytes that stay put for it, and new
+    tensors of 77 that must stay as they are."""
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    before = _held()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    kept = call(side)
+    held = _held() - before
+    new = [torch.full((n,), 77, dtype=torch.int32, device="cuda") for n in (1 << 19, 1 << 19, 1 << 17, 1 << 17, 4096, 4096, 128, 128)]
+    torch.cuda.synchronize()
+    assert all((t == 77).all() for t in new)
+    return kept, held
+
+
+def test_norm_results_that_are_let_go_of():
+    T, H = 4096, 512     # large enough for storages of their own
+    g = torch.Generator("cuda").manual_seed(5)
+    x, w = torch.randn(T, H, device="cuda", generator=g).bfloat16(), torch.ones(H, device="cuda")
+    want = b.dvp_rms_norm(x, w, residual=x, out_dtype=torch.float8_e4m3fn)
+    kept, held = _behind_a_busy_stream(lambda s: b.dvp_rms_norm(x, w, residual=x, out_dtype=torch.float8_e4m3fn, stream=s).y)
+    assert held >= T * 4 + T * 4 * 4 + T * H * 2     # rstd, scale, residual
+    assert torch.equal(kept.view(torch.uint8), want.y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("T", [2, 3000])
+def test_rollout_head_whose_product_is_refused(T):
+    H = 1024
+    x, gamma = torch.randn(T, H, device="cuda").bfloat16(), torch.ones(H, device="cuda")
+    q = b.dvp_quantize_fp8(torch.randn(500, H // 2, device="cuda"))     # of another width
+
+    def call(side):
+        try:
+            b.dvp_rollout_head(x, gamma, q.q, q.scale, torch.rand(T, device="cuda"), stream=side)
+        except ValueError:
+            return True
+    refused, held = _behind_a_busy_stream(call)
+    assert refused and held >= T * H
