@@ -842,6 +842,9 @@ def dvp_quantize_fp8(x: torch.Tensor, *, block_rows: int = FP8_BLOCK, stream=Non
     rows, cols = x.shape
     q = x.new_empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn)[:, :cols]
     scale = x.new_empty((-(-rows // block_rows), -(-cols // FP8_BLOCK)), dtype=torch.float32)
+    if stream is not None:  # their memory stays put until the stream is through with it, whoever lets go of them before
+        q.record_stream(stream)
+        scale.record_stream(stream)
     with _on_device_of(x):
         st = packed["dvp_quantize_fp8"](_QUANTIZE_FP8_PACK.pack(
             _QUANTIZE_FP8_PACK.size, _DTYPES[x.dtype], rows, cols, x.stride(0), q.stride(0), scale.stride(0), x.data_ptr(),

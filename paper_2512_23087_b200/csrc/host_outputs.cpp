@@ -433,6 +433,8 @@ PyObject *rms_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n_args
   a.d_x = d_x.data_ptr(), a.ld_d_x = H;
   const at::Tensor d_weight = given(args[7]) ? vector(args[7], "d_weight", H, at::kFloat, at::kFloat, h) : made.take(H, -1, 0, at::kFloat);
   a.d_weight = static_cast<float *>(d_weight.data_ptr());
+  keep_for(d_x, args[10]);
+  if (!given(args[7])) keep_for(d_weight, args[10]);
   at::Tensor workspace;
   if (given(args[9])) {
     workspace = tensor(args[9], "workspace");
@@ -485,7 +487,10 @@ PyObject *gemm_fp8(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   }
   const at::ScalarType type = given(args[6]) ? out.scalar_type() : type_of(args[5]);
   const int32_t code = code_of(type, "out");
-  if (!out.defined()) out = make(x, {M, N}, type);
+  if (!out.defined()) {
+    out = make(x, {M, N}, type);
+    keep_for(out, args[7]);
+  }
   const at::Tensor status = make(x, {1}, at::kInt);
   keep_for(status, args[7]);  // callers let go of it at once
   if (M == 0 || N == 0) {  // no kernel runs that would say that none has given up
@@ -559,6 +564,7 @@ PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   if (PyErr_Occurred()) throw python_error();
   // rows 0 to 3 of the storage: three vectors of 4 bytes a token; behind them the ids
   Vectors v(z, T, 5);
+  keep_for(v.buf, args[8]);
   THPObjectPtr d(PyDict_New());
   if (!d) throw python_error();
   put(d.get(), g_names.logp, v.make(0, at::kFloat, &a.logp));

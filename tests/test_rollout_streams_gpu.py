@@ -134,3 +134,21 @@ def test_rollout_head_whose_product_is_refused(T):
             return True
     refused, held = _behind_a_busy_stream(call)
     assert refused and held >= T * H
+
+
+def test_other_results_that_are_let_go_of():
+    T, H, V = 4096, 1024, 2048
+    g = torch.Generator("cuda").manual_seed(6)
+    h, w = torch.randn(T, H, device="cuda", generator=g), torch.ones(H, device="cuda")
+    rstd, u = h.square().mean(1).rsqrt(), torch.rand(T, device="cuda", generator=g)
+    want = b.dvp_rms_norm_backward(h, h, w, rstd)
+    kept, held = _behind_a_busy_stream(lambda s: b.dvp_rms_norm_backward(h, h, w, rstd, stream=s).d_weight)
+    assert held >= T * H * 4 and torch.equal(kept, want.d_weight)
+    kept, held = _behind_a_busy_stream(lambda s: b.dvp_quantize_fp8(h, stream=s).scale)
+    assert held >= T * H and torch.equal(kept, b.dvp_quantize_fp8(h).scale)
+    _, held = _behind_a_busy_stream(lambda s: (b.dvp_sample(h, u, stream=s), None)[1])
+    assert held >= T * 20
+    q = b.dvp_quantize_fp8(h, block_rows=1)
+    k = b.dvp_quantize_fp8(torch.randn(V, H, device="cuda", generator=g))
+    _, held = _behind_a_busy_stream(lambda s: (b.dvp_gemm_fp8(q.q, q.scale, k.q, k.scale, stream=s), None)[1])
+    assert held >= T * V * 2
