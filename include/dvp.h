@@ -701,8 +701,9 @@ int dvp_sample(const dvp_sample_args *args);
 
 /*
  * Bytes of device workspace the entry point needs for `args` (a pointer to
- * that entry point's args struct; only sizes and dtypes are read).  Returns 0
- * for entry points that need none and for invalid arguments.
+ * that entry point's args struct; only sizes and dtypes are read, and for
+ * DVP_ENTRY_RMS_NORM_BACKWARD whether d_weight is NULL: without it the call needs
+ * none).  Returns 0 for entry points that need none and for invalid arguments.
  */
 size_t dvp_workspace_bytes(int entry_point, const void *args);
 
