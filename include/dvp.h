@@ -656,8 +656,10 @@ int dvp_gemm_fp8(const dvp_gemm_fp8_args *args);
  *        K1 for top_p >= 1)
  * where equal logits stand in the order of their indices, and the token is the first a in K2 with
  *   sum_{k in K2, k <= a} w_k > uniform * sum_{k in K2} w_k        (the indices' order; the last with w > 0 where none is)
- * Sums and the decisions that rest on them are formed in double: the token is that of exact arithmetic unless `uniform` lies
- * within some 1e-12 of a border.  Temperature 0 takes the largest logit (the first of equals): K2 has one token.
+ * Decisions are those of sums in double, formed as such, or in float32 where a bound on its errors says that they decide alike: the
+ * token is that of exact arithmetic unless `uniform` lies within some 1e-12 of a border.  The sum in logp, and that in logp_mp where
+ * it decided, has float32 terms: it is off by a few 1e-6 of what it has beside the maximum's own term.  Temperature 0 takes the
+ * largest logit (the first of equals): K2 has one token.
  *
  *   logits        device [T, ld] of logits_dtype (DVP_F32, DVP_BF16, DVP_F16), any stride and alignment to its element.
  *                 -inf marks tokens that are not to be drawn

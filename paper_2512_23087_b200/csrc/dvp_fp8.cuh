@@ -35,8 +35,8 @@ static __device__ __noinline__ uint32_t divided(float a, float b, float c, float
 // Eight or four quotients.  The conversion is monotone, so where products with a bound of 1 / c on either side become the same value, the
 // quotient does too: the special-function unit's reciprocal is good to 2^-23, two roundings on the way add 2^-24 each, and the
 // quotient's own is one more, less than the 2^-21 between the bounds and it.  Only what lies so near a border is divided:
-// about one four in twenty thousand (16,384 x 4,096 bfloat16, norm to 8 bits: 113 us; with a division each 134; with products by an
-// approximate reciprocal alone, which put some values on the border's other side, 105).
+// one four in some twenty thousand (16,384 x 4,096 bfloat16, norm to 8 bits: 111 us; with a division each 131; with products by the
+// approximate reciprocal alone, which put some values on the border's other side, 102).
 template <int N>
 __device__ __forceinline__ void quotients(const float (&y)[N], float c, uint32_t (&q)[N / 4]) {
   float r;

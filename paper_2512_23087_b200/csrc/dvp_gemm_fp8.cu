@@ -103,7 +103,7 @@ __device__ __forceinline__ void store16(TC *c, const float *v, int n, bool vec) 
 // scheduler, 256, and tensor memory is read beside them: the next 32 columns while 32 are added.  For that the epilogue's warps
 // take over registers of the others: 168 a thread at launch, 56 and 224 then, which is the same sum.
 //
-// Bound by the reading back: the tensor cores are busy 47 % of the time.  4,096 x 4,096 x 151,936 to bfloat16: 2,740 us by itself
+// Bound by the waits of the reading back: tensor cores busy 44 % of the cycles, tensor memory 55 % (18,944 rows of B).  4,096 x 4,096 x 151,936 to bfloat16: 2,740 us by itself
 // (1,860 TFLOP/s), some 3,150 in a row of calls, where the board's power lowers the clock.  Slower were packed multiply-adds
 // (3,008 us), four accumulators of 128 columns (3,316), sixteen epilogue warps (3,037), one lane that waits for its warp (2,759).
 constexpr int kThreads8 = 384;
@@ -313,7 +313,8 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 // 128 were 1,187 tiles for 148 blocks, nine for some and eight for most); rows of the instruction behind them compute on
 // what the ring held before, and nobody reads their sums.
 // Warp 0: TMA, warp 1: MMA, the others: epilogue, a row of B and up to 32 tokens a thread.
-// Bound by HBM: 16 x 4,096 x 151,936 takes 111 us, 627 MB at 5.65 TB/s (64 tokens 144 us).
+// Bound by HBM: 16 x 4,096 x 151,936 takes 110 to 118 us, 627 MB at 5.3 to 5.7 TB/s.  64 tokens 135 to 144 us, floor 98: a stage of four
+// slices is 98 KB then, so that the ring has two.
 constexpr int kSlicesPerStage = 4;  // a row of B is asked for in so many times 128 bytes (16 x 4,096 x 151,936: 111 us, with two 117)
 
 template <int NT>
@@ -490,7 +491,8 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 // ---- the quantiser -----------------------------------------------------------------------------------------------------
 // q = e4m3(x / c), c = max(max |x|, 2^-96) / 448 over a block.  A block of threads takes 128 rows x 128 columns, a warp 16 of the
 // rows, a lane four neighbouring columns, all of it in registers, so that the matrix is read once; kRowScale: every row has a
-// scale of its own.  For weights, which are quantised once.
+// scale of its own.  151,936 x 4,096 bfloat16: 1,534 us, 1.2 TB/s (floor 284), by rows 1,904; one block of 256 threads loads, then
+// computes, then stores its 128 x 128, and at 128 registers a thread two of them share an SM.
 template <typename T, bool kRowScale>
 __global__ void __launch_bounds__(256) quantize_kernel(const T *x, long long ld_x, uint8_t *out, long long ld_out, float *scale,
                                                        long long ld_scale, long long rows, long long cols, int vec) {
@@ -627,7 +629,7 @@ cudaError_t launch_few(const dvp_gemm_fp8_args *a, Params8 p, int sms, cudaStrea
   return cudaGetLastError();
 }
 
-// By the tokens: B is read once either way, but of pair tiles a few tokens fill only a part (64 x 4,096 x 151,936: 144 us, by
+// By the tokens: B is read once either way, but of pair tiles a few tokens fill only a part (64 x 4,096 x 151,936: 135 to 144 us, by
 // pairs 198 to 204, which is what 128 tokens take; 128 tokens with swapped operands were 284).
 template <typename TC>
 cudaError_t launch(const dvp_gemm_fp8_args *a, const Params8 &p, int sms, cudaStream_t stream) {

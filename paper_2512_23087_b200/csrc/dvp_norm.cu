@@ -18,7 +18,7 @@ namespace norm {
 
 constexpr int kBlockCols = 128;  // columns that share a scale
 constexpr int kVec = 8;          // elements of a vector: 16 bytes of a 16-bit type, 32 of float32, 8 of e4m3
-constexpr int kMaxPartials = 592;               // rows of partial sums of dw: four blocks an SM
+constexpr int kMaxPartials = 592;               // rows of partial sums of dw: one a block and row side by side, for 148 SMs four an SM
 
 struct Params {
   const void *x, *r, *w;
@@ -118,7 +118,8 @@ __device__ __forceinline__ float row_sum(float v, int tpr, float *part) {
 // ---- rows in vectors ---------------------------------------------------------------------------------------------------
 
 // A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: the next is on its way while one is summed up and stored, so that loads
-// never pause (16,384 x 4,096 bfloat16 to 8 bits, quotients aside: 103 us, with one row a block and nothing on its way 139).
+// never pause (16,384 x 4,096 bfloat16 to 8 bits, with approximate quotients and roots: 103 us, with one row a block and nothing on its
+// way 139; as it is now 113, 4.2 TB/s: instructions issue in 0.59 of the cycles, and warps wait for loads and for the row's chain).
 template <typename T, typename TOut, int kPer>
 __global__ void __launch_bounds__(kPer == 4 ? 512 : 256, kPer == 1 ? 4 : kPer == 2 ? 3 : 1) rms_norm_kernel(const Params p, const int tpr) {
   __shared__ __align__(16) float part[2][32];
@@ -229,8 +230,8 @@ __device__ __forceinline__ float block_sum(float v, float *part) {
 }
 
 // A warp takes whole blocks of 128 columns, four a lane, in both sweeps alike: what takes an input's place is written by the
-// thread that has read it last.  (Kept in registers between the sweeps, 32 a thread, the rows were slower: 1,111 x 5,003 float16 16.4 us
-// a call, read twice 12.3, as twice as many blocks fit an SM.)
+// thread that has read it last.  (Kept in registers between the sweeps, 32 a thread, the rows were slower on one box: 1,111 x 5,003 float16
+// 16.4 us a call, read twice 12.3, as twice as many blocks fit an SM.  In a row of calls over three states it takes 14.4 to 14.7.)
 template <typename T, typename TOut>
 __global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params p) {
   __shared__ float part[kAnyThreads / 32];
@@ -296,8 +297,10 @@ struct BackParams {
 };
 
 // A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: its threads keep their columns, and with them the sums of dw.  Bound by
-// HBM: 16,384 x 4,096 bfloat16 with float32 dy, dr and dw 122 us, 671 MB at 5.5 TB/s; without the next row on its way 166, with its
+// HBM: 16,384 x 4,096 bfloat16 with float32 dy, dr and dw 122 to 131 us, 671 MB at 5.1 to 5.5 TB/s; without the next row on its way 166, with its
 // addresses formed anew for each row 131.  The sum of the partial rows is a launch of its own, some 5 us of a call's.
+// Four vectors a thread (8,200 to 16,384 columns) spill some 600 bytes at 128 registers: 4,096 x 16,384 198 us, 3.4 TB/s.  Rows of up
+// to 256 columns lie eight a block side by side, and the workspace's 592 rows allow 74 such blocks: 32,768 x 128 42 us, 1 TB/s.
 template <typename T, typename TD, int kPer>
 __global__ void __launch_bounds__(512, kPer == 1 ? 2 : 1) rms_norm_backward_kernel(const BackParams p, const int tpr) {
   __shared__ __align__(16) float part[2][32];
@@ -438,7 +441,7 @@ inline bool weight_vectors(const void *w) { return (uintptr_t)w % 16 == 0; }
 struct Shape {
   int per, tpr, rpb;  // vectors a thread, threads a row, rows a block
 };
-// Forward, one vector a thread up to 256 threads a row, then two (16,384 x 4,096 to 8 bits, quotients aside: 103 us, one vector and 512 threads
+// Forward, one vector a thread up to 256 threads a row, then two (16,384 x 4,096 to 8 bits, approximate quotients: 103 us, one vector and 512 threads
 // 114), then four; backward, whose threads hold a row of dw too, 512.  per = 0: too long for the registers, or no vector at all.
 inline Shape shape_of(long long H, bool backward) {
   const long long nv = H / kVec;

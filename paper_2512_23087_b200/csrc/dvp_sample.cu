@@ -2,8 +2,8 @@
 // of their mass, at a temperature, by a given random number.
 //
 // Every one of the three filters keeps the front of the row in falling order (equal logits by index), so what is kept is one
-// cut: the logits above a value `v` and, of those equal to it, the ones up to an index.  Nothing is sorted but a few hundred
-// logits around the cut:
+// cut: the logits above a value `v` and, of those equal to it, the ones up to an index.  Nothing is sorted but the logits around the
+// cut, 2,048 at most:
 //
 //   1  the row streams past once: its maximum, the sum of e^{(z - m) / T} without the maximum's own terms (so that ln of the whole
 //      sum keeps its digits where one token has all the mass), a sum for each piece of the row, and the maximum of each 32-byte
@@ -19,8 +19,9 @@
 // is tried first: it is good to error(), and mostly nothing lies so near the border that this matters.  With few rows the blocks
 // of a cluster share a row and exchange sums through shared memory.
 //
-// Bound by instruction issue (three cycles of five) and by the waits of a row's phases, not by HBM: 1,024 rows of 151,936 bfloat16 (311 MB, 47 us at 6.6 TB/s)
-// take 122 us for the largest logit, 173 with nothing cut, 334 with a min-p set of 80 % of the row, 307 with top_k 50 and 529 with
+// Bound by instruction issue (three cycles of five) and by the waits of a row's phases, not by HBM; at 64 registers a thread, which two
+// blocks an SM want, some 850 bytes a thread are spilled.  1,024 rows of 151,936 bfloat16 (311 MB, 47 us at 6.6 TB/s)
+// take 122 us for the largest logit, 173 to 182 with nothing cut, 334 to 339 with a min-p set of 80 % of the row, 307 with top_k 50 and 529 to 538 with
 // top_p 0.95, whose rows are read four times, once only a quarter of them.  Of a top_p row's some 200 thousand cycles, two
 // rows an SM, the first sweep has 50, the quarter's histogram and its window 33, the sum behind the window with its list 80, the sort
 // 20.  One row of that length takes 19 to 50 us by eight blocks.
@@ -1646,7 +1647,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
 
 // ---- host --------------------------------------------------------------------------------------------------------------
 
-// Blocks that share a row.  More of them shorten the sweeps and lengthen what they do together, and clusters of eight find room
+// Blocks that share a row; the limits are those of a chip of 148 SMs.  More of them shorten the sweeps and lengthen what they do together, and clusters of eight find room
 // for fewer of them at a time.  1 / 2 / 4 / 8 blocks a row, us a call, of bfloat16:
 //   4 x 151,936, top_p 0.95    110 / 78 / 55 / 51       74 x 151,936, top_p 0.95   226 / 142 / 127 / 185
 //   64 x 151,936, nothing cut   71 / 52 / 36 / 42       148 x 151,936, top_k 50     65 / 76 / 171 / 287
