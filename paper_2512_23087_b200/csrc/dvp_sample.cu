@@ -942,14 +942,21 @@ struct Row {
       if (guess) edges(sh()->pick_lo, sh()->pick_hi, per, low, high);
       meet();  // the histograms have been read
     }
-    // every level divides the keys by 2,048, at the latest from the eighth on: eleven are the most
+    // Bounds by the bins' edges need not say where among many bins the cut lies (an aim next to the sum of what lies far in front of the
+    // rest, say), and say no more at the next level.  That one is for the lower half of the bins then, from `half` down, and its
+    // sum of what lies above says whether the cut is there at all.
+    bool halve = false;
+    float half = 0.f;
+    // from the second level on every one divides the keys by 64, or the next one by 2: 2^32 of them want fewer than 70
 #pragma unroll 1
-    for (int level = guess ? 1 : 0; level < 16; ++level) {
+    for (int level = guess ? 1 : 0; level < 70; ++level) {
+      const float top = high;
+      if (halve) high = half;
       const uint32_t k_lo = key_of(low), k_hi = key_of(high), width = k_hi - k_lo;
       const int shift = max(0, 21 - __clz(width));  // (width >> shift) < kBins
       const bool gather = level > 0 && n_in <= kList;
       // where the bracket has one value, its logits are taken by their index
-      const bool ties = level > 0 && !gather && width == 0;
+      const bool ties = level > 0 && !gather && width == 0 && !halve;
       if (level == 2 && !gather && unsure > 0.0) {  // a flat row: bins of single values want the aim itself
         all = whole();
         aim = share * all;
@@ -980,6 +987,14 @@ struct Row {
         sums = sum(a);
         replaced = true;
         above = weights ? sums.all : (double)sums.n;
+      }
+      if (halve) {
+        halve = false;
+        if (above >= aim) {
+          low = value_of(k_hi + 1);
+          high = top;
+          continue;
+        }
       }
       if (ties) {
         // kept are the first r with above + (r - 1) w < aim
@@ -1096,6 +1111,8 @@ struct Row {
       } else {
         low = fmaxf(low, value_of(edge_of(k_lo, k_hi, hi, shift)));
         high = value_of(k_hi - (lo << shift));
+        halve = weights && unsure == 0.0 && shift > 0 && hi - lo >= kBins / 64 && n_in > kList;
+        half = value_of(edge_of(k_lo, k_hi, (lo + hi) / 2, shift) - 1);
       }
     }
     return kStale;
@@ -1297,8 +1314,8 @@ struct Row {
   __device__ void bracket(bool weights, int level, double aim, double above, double all, double unsure, double below, double all_unsure, float per,
                           uint32_t k_lo, uint32_t k_hi, int shift) {
     constexpr int kOwn = kBins / kThreads;
-    // where a bin holds one value, or the bracket would not get smaller, the larger bound decides
-    const bool sharp = !weights || level >= 8 || (level > 1 && shift == 0);
+    // where a bin holds one value, its bounds are one
+    const bool sharp = !weights || (level > 1 && shift == 0);
     uint32_t n[kOwn];
     double least[kOwn], most[kOwn], least_sum = 0.0, most_sum = 0.0;
     bins_of_row(n);
@@ -1369,7 +1386,7 @@ struct Row {
       if (last_any) atomicMax(&sh()->pick_last, last_any);
     }
     __syncthreads();
-    uint32_t lo = sh()->pick_lo, hi = min(sh()->pick_hi, (uint32_t)kBins - 1);
+    uint32_t lo = sh()->pick_lo, hi = min(sh()->pick_hi, sh()->pick_last);
     if (level > 0 && lo == kBins) lo = hi = sh()->pick_last;  // the cut is in the bracket: what is missing is a rounding
     // logits in bins lo to hi
     uint32_t inside = 0;
