@@ -1620,8 +1620,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const Params p) {
         double unsure = 0.0, behind = 0.0;
         if (have != Row<T>::kStale) {
           all = row.sum_of_chunks();
-          // a logarithm near zero wants all of its sum's digits
-          if (have == Row<T>::kTail && !was_whole && !(all > 1.5)) {
+          // a logarithm near zero wants all of its sum's digits, and a small part of the row has the whole row's errors
+          if (have == Row<T>::kTail && !was_whole && !(all > 1.5 && row.error(rest + 1.0) + row.error(rest + 1.0 - all) < 4e-6 * all)) {
             have = Row<T>::kStale;
             continue;
           }
