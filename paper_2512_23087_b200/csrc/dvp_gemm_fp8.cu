@@ -130,6 +130,14 @@ __device__ __forceinline__ void give_up(volatile int *abort_flag, int *status, i
   }
 }
 
+// The producer's last act: waits until the products of the last stages have handed them back, so that no arrival is on its way to a
+// barrier of a block that has ended.  `n` stages were filled, one hand-over each.
+template <int kStages>
+__device__ __forceinline__ void wait_for_last(const uint64_t (&empty)[kStages], uint32_t n, volatile int *abort_flag, int *status) {
+  for (uint32_t it = n > kStages ? n - kStages : 0; it < n && !*abort_flag; ++it)
+    if (!mbar_wait(smem_u32(&empty[it % kStages]), (it / kStages) & 1, abort_flag)) give_up(abort_flag, status, kErrProducerWait);
+}
+
 template <typename TC>
 __global__ void __launch_bounds__(kThreads8, 1)
 gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Params8 p) {
@@ -188,6 +196,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           tma_load_2d_pair(dst + kBytesA8, &map_b, bar, ks * kBlock, tn * 256 + (int)rank * 128);
         }
       }
+      wait_for_last(sh->empty, it, abort_flag, p.status);
     } else if (warp == 1 && lane == 0 && rank == 0) {
       const uint32_t idesc = instr_desc8(256, 256);
       uint32_t it = 0;
@@ -388,6 +397,7 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
           for (int h = 0; h < n; ++h) tma_load_2d(dst + h * F::kSlice, &map_b, bar, (ks + h) * kBlock, tile * p.tile_rows);
           for (int h = 0; h < n; ++h) tma_load_2d(dst + h * F::kSlice + F::kBytesB, &map_x, bar, (ks + h) * kBlock, 0);
         }
+      wait_for_last(sh->empty, it, abort_flag, p.status);
     }
   } else if (warp == 1) {
     if (lane == 0) {
