@@ -522,10 +522,10 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T *x, long long ld_
     const T *p = x + r * ld_x + c;
     if (whole) {
       if constexpr (sizeof(T) == 4) {
-        const float4 q = __ldg(reinterpret_cast<const float4 *>(p));
+        const float4 q = *reinterpret_cast<const float4 *>(p);  // not by __ldg, which may be executed ahead of its checks
         v[i][0] = q.x, v[i][1] = q.y, v[i][2] = q.z, v[i][3] = q.w;
       } else {
-        const uint2 q = __ldg(reinterpret_cast<const uint2 *>(p));
+        const uint2 q = *reinterpret_cast<const uint2 *>(p);
         const T *e = reinterpret_cast<const T *>(&q);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i][j] = Storage<T>::widen(e[j]);

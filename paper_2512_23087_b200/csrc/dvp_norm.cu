@@ -70,20 +70,21 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
     store_grads<T, 8>(p, v);
   }
 }
-// Weights: read by every row, so they stay in L1.
+// Weights: read by every row, so they stay in L1.  Loads by __ldg, which promises that nothing writes there, were executed ahead of
+// the comparison with the row's end: a float32 weight of one element was read by a whole block.  Ordinary loads are not.
 template <typename T>
 __device__ __forceinline__ void load_weights8(const void *w, int w_f32, long long c, float (&v)[8]) {
   if (sizeof(T) == 4 || w_f32) {
     const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(w) + c);
-    const float4 a = __ldg(q), b = __ldg(q + 1);
+    const float4 a = q[0], b = q[1];
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
   } else if constexpr (sizeof(T) == 2) {
-    Storage<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(w) + c)), v);
+    Storage<T>::unpack(*reinterpret_cast<const uint4 *>(static_cast<const T *>(w) + c), v);
   }
 }
 template <typename T>
 __device__ __forceinline__ float load_weight(const void *w, int w_f32, long long c) {
-  return sizeof(T) == 4 || w_f32 ? __ldg(static_cast<const float *>(w) + c) : Storage<T>::widen(__ldg(static_cast<const T *>(w) + c));
+  return sizeof(T) == 4 || w_f32 ? static_cast<const float *>(w)[c] : Storage<T>::widen(static_cast<const T *>(w)[c]);
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
