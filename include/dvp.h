@@ -526,7 +526,7 @@ int dvp_debug_bounds_status(uint32_t *status_out);
  *
  * dvp_rms_norm -- root-mean-square norm, with the residual's addition:
  *   h = x + residual,  s = (mean_j h_j^2 + eps)^(-1/2),  y_j = h_j s weight_j
- * in float32 from the stored values; every output is rounded once.
+ * in float32 from the stored values; every output is rounded once.  With eps = 0 a row of zeros has s infinite and y NaN.
  *
  *   x, residual   device [T, ld] of x_dtype; residual may be NULL
  *   weight        device [H] of x_dtype or DVP_F32 (weight_dtype)

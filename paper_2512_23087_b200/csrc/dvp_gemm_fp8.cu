@@ -501,7 +501,7 @@ gemm_fp8_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 // ---- the quantiser -----------------------------------------------------------------------------------------------------
 // q = e4m3(x / c), c = max(max |x|, 2^-96) / 448 over a block.  A block of threads takes 128 rows x 128 columns, a warp 16 of the
 // rows, a lane four neighbouring columns, all of it in registers, so that the matrix is read once; kRowScale: every row has a
-// scale of its own.  151,936 x 4,096 bfloat16: 1,534 us, 1.2 TB/s (floor 284), by rows 1,904; one block of 256 threads loads, then
+// scale of its own.  151,936 x 4,096 bfloat16: 1,526 us, 1.2 TB/s (floor 284), by rows 1,888; one block of 256 threads loads, then
 // computes, then stores its 128 x 128, and at 128 registers a thread two of them share an SM.
 template <typename T, bool kRowScale>
 __global__ void __launch_bounds__(256) quantize_kernel(const T *x, long long ld_x, uint8_t *out, long long ld_out, float *scale,

@@ -231,8 +231,8 @@ __device__ __forceinline__ float block_sum(float v, float *part) {
 }
 
 // A warp takes whole blocks of 128 columns, four a lane, in both sweeps alike: what takes an input's place is written by the
-// thread that has read it last.  (Kept in registers between the sweeps, 32 a thread, the rows were slower on one box: 1,111 x 5,003 float16
-// 16.4 us a call, read twice 12.3, as twice as many blocks fit an SM.  In a row of calls over three states it takes 14.4 to 14.7.)
+// thread that has read it last.  (Kept in registers between the sweeps, 32 a thread, the rows were slower: 1,111 x 5,003 float16 16.4 us a
+// call, read twice 12.3, as twice as many blocks fit an SM.)
 template <typename T, typename TOut>
 __global__ void __launch_bounds__(kAnyThreads) rms_norm_any_kernel(const Params p) {
   __shared__ float part[kAnyThreads / 32];
@@ -300,8 +300,8 @@ struct BackParams {
 // A block's rows are blockIdx.x * rpb + i * gridDim.x * rpb: its threads keep their columns, and with them the sums of dw.  Bound by
 // HBM: 16,384 x 4,096 bfloat16 with float32 dy, dr and dw 122 to 131 us, 671 MB at 5.1 to 5.5 TB/s; without the next row on its way 166, with its
 // addresses formed anew for each row 131.  The sum of the partial rows is a launch of its own, some 5 us of a call's.
-// Four vectors a thread (8,200 to 16,384 columns) spill some 600 bytes at 128 registers: 4,096 x 16,384 198 us, 3.4 TB/s.  Rows of up
-// to 256 columns lie eight a block side by side, and the workspace's 592 rows allow 74 such blocks: 32,768 x 128 42 us, 1 TB/s.
+// Four vectors a thread (8,200 to 16,384 columns) spill some 600 bytes at 128 registers: 4,096 x 16,384 192 us, 3.5 TB/s.  Rows of up
+// to 256 columns lie eight a block side by side, and the workspace's 592 rows allow 74 such blocks: 32,768 x 128 44 us, 1 TB/s.
 template <typename T, typename TD, int kPer>
 __global__ void __launch_bounds__(512, kPer == 1 ? 2 : 1) rms_norm_backward_kernel(const BackParams p, const int tpr) {
   __shared__ __align__(16) float part[2][32];

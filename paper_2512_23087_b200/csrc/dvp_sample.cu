@@ -20,8 +20,8 @@
 // of a cluster share a row and exchange sums through shared memory.
 //
 // Bound by instruction issue (three cycles of five) and by the waits of a row's phases, not by HBM; at 64 registers a thread, which two
-// blocks an SM want, some 850 bytes a thread are spilled.  1,024 rows of 151,936 bfloat16 (311 MB, 47 us at 6.6 TB/s)
-// take 122 us for the largest logit, 173 to 182 with nothing cut, 334 to 339 with a min-p set of 80 % of the row, 307 with top_k 50 and 529 to 538 with
+// blocks an SM want, some 870 bytes a thread are spilled.  1,024 rows of 151,936 bfloat16 (311 MB, 47 us at 6.6 TB/s)
+// take 122 us for the largest logit, 173 to 182 with nothing cut, 334 to 339 with a min-p set of 80 % of the row, 307 with top_k 50 and 518 to 540 with
 // top_p 0.95, whose rows are read four times, once only a quarter of them.  Of a top_p row's some 200 thousand cycles, two
 // rows an SM, the first sweep has 50, the quarter's histogram and its window 33, the sum behind the window with its list 80, the sort
 // 20.  One row of that length takes 19 to 50 us by eight blocks.
